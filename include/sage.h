@@ -19,7 +19,8 @@
  *  - `status` (int32_t[1], device, may be NULL) receives the first data-dependent
  *    error a kernel meets (SAGE_STATUS_*); kernels then return early and never
  *    trap.  The caller zeroes it and reads it back when it wants to.
- *  - Inputs are never modified, except by sage_compact_kv (pools, seq_len).
+ *  - Inputs are never modified, except by sage_compact_kv (pools, seq_len), sage_rope_append (pools) and
+ *    sage_seal_kv (sealed cache, sealed).
  *  - Results are deterministic run to run.
  *  - Trees: node_offsets[batch+1] delimits each sequence's nodes; within a tree
  *    node 0 is the root (the last committed token, parent = -1) and every other
@@ -30,6 +31,8 @@
  *    sequence b lives in page page_table[b*max_pages_per_seq + t/page_size], slot
  *    t%page_size.  seq_len[b] = prefix length L_b; the K/V of the N_b tree nodes
  *    sit at logical positions L_b .. L_b+N_b-1 of the same cache.
+ *  - Sealed pages (sage_seal_kv, sage_tree_attention_sealed): a second cache of 8 bits holds pages that are full, see
+ *    sage_sealed_cache.
  *  Supported envelope (else SAGE_ERR_UNSUPPORTED): head_dim = 128, page_size = 64,
  *  n_q_heads / n_kv_heads in {1,2,4,8}, k <= 16, k_entropy <= 16, finite logits.
  */
@@ -242,6 +245,92 @@ int sage_compact_kv(void *k_pool, void *v_pool, int64_t layer_stride_elems, int 
                     const int32_t *page_table, int max_pages_per_seq, int32_t *seq_len,
                     const int32_t *path, const int32_t *path_len, int batch, int max_path,
                     int n_kv_heads, int head_dim, int page_size, int32_t *status, void *stream);
+
+/* Tree attention with a window: as sage_tree_attention, but a row sees only the last `window` positions and the first `n_sink`
+ * ones.  The tree node i stands at position pi = L_b + depth(i) (the root has depth 0), a key of the prefix at its logical position,
+ * a node j of the tree at L_b + depth(j); of what sage_tree_attention would let node i see, the keys at positions kappa with
+ * pi - kappa < window or kappa < n_sink remain (its own always).  window >= 1, n_sink >= 0; a window of L_b + 64 or more takes nothing away.
+ * Only pages that hold such a key are read: page_table entries of the others are not looked at.
+ * Softmax and accumulation in fp32, probabilities rounded to bf16.  ws: sage_tree_attention_window_workspace_size(...)
+ * bytes, for the same sizes.  One or two launches. */
+int sage_tree_attention_window(const void *q, const void *k_pool, const void *v_pool,
+                               int64_t layer_stride_elems, int n_layers, int n_pages,
+                               const int32_t *page_table, int max_pages_per_seq, const int32_t *seq_len,
+                               const int32_t *parent, const int32_t *node_offsets, int batch, int sum_nodes,
+                               int n_q_heads, int n_kv_heads, int head_dim, int page_size, float sm_scale,
+                               int window, int n_sink,
+                               void *out, void *ws, size_t ws_bytes, int32_t *status, void *stream);
+size_t sage_tree_attention_window_workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads,
+                                                 int head_dim, int max_pages_per_seq, int window, int n_sink);
+
+/* Rotary positions with up to three axes (time, height, width), and the way of new keys and values into the cache.
+ * Rows are bf16 [layer][token][head][128]; heads lie side by side, layers and tokens at the given distances (elements, multiples of
+ * 8; so q, k and v may be parts of the rows of one projection).  The tokens of sequence b are node_offsets[b] .. node_offsets[b+1]-1
+ * (any number of them, none included), its next places in the cache L_b, L_b + 1, ... (seq_len is not changed: what is appended counts as the tree's rows
+ * until sage_compact_kv, or the caller after a prefill, advances it).  For i < 64 the pair (x[i], x[i+64]) of every
+ * query and key head turns by the angle pos[axis[i]] * inv_freq[i]:
+ *   x'[i] = scale * (x[i] cos - x[i+64] sin),  x'[i+64] = scale * (x[i+64] cos + x[i] sin),
+ * angles reduced in 64 bits, products in fp32, rounded once to bf16.  Turned queries go to q_out
+ * (bf16 [n_layers][sum_tokens][n_q_heads][128], as sage_tree_attention reads them; it may be q itself where q lies like that, else
+ * it is apart from all inputs), turned keys and unchanged values to their places in the pools.
+ * Positions: pos int32 [3][sum_tokens], or, with pos == NULL, from the tree: node i of sequence b has next_pos[b] + depth(i)
+ * on all axes (parent as everywhere; at most 64 nodes; parent and next_pos are NULL otherwise).  Rows behind the last sequence are left as they are.  A sequence
+ * that does not fit its page table is reported in `status` and left out; so are keys and values of a token whose page id is out of range.  One launch. */
+typedef struct sage_rope_rows {
+    const void *q, *k, *v;
+    int64_t q_layer_stride, q_token_stride, k_layer_stride, k_token_stride, v_layer_stride, v_token_stride;
+} sage_rope_rows;
+typedef struct sage_rope_policy {
+    double  inv_freq[64];   /* radians per position: base^(-i/64), or scaled as the model asks; magnitude up to 1e6 */
+    uint8_t axis[64];       /* which of the three positions: 0 time, 1 height, 2 width */
+    float   scale;          /* of the turned rows: 1, or the model's factor for stretched contexts */
+} sage_rope_policy;
+int sage_rope_append(const sage_rope_rows *rows, const sage_rope_policy *policy /* host, both */,
+                     int n_layers, int sum_tokens, int n_q_heads, int n_kv_heads, int head_dim,
+                     const int32_t *pos, const int32_t *parent, const int32_t *next_pos,
+                     void *q_out, void *k_pool, void *v_pool, int64_t layer_stride_elems, int n_pages, int page_size,
+                     const int32_t *page_table, int max_pages_per_seq, const int32_t *seq_len,
+                     const int32_t *node_offsets, int batch, int32_t *status, void *stream);
+
+/* A cache of 8 bits for pages that are full (host struct, device pointers).  k, v: e4m3 [n_layers][n_pages][n_kv_heads][64][128],
+ * layers layer_stride bytes apart; k_exp, v_exp: [n_layers][n_pages][n_kv_heads], one byte for each page and KV head: a value
+ * stands for itself times 2^(byte - 127), byte in 67 .. 187 (one outside is read as the nearest).  page_table: as everywhere, ids of these pools,
+ * max_pages_per_seq entries per sequence.  `sealed`[b] (given beside it) is how many of sequence b's first pages are held here; they no longer need
+ * a place in the bf16 pools, whose page table is not read for them (entry p may name the page of entry p + 4, say). */
+typedef struct sage_sealed_cache {
+    void *k, *v;
+    int64_t layer_stride;
+    uint8_t *k_exp, *v_exp;
+    int n_pages;
+    const int32_t *page_table;
+    int max_pages_per_seq;
+} sage_sealed_cache;
+
+/* Seals every page of the prefix that is full and not sealed yet: pages sealed[b] .. seq_len[b]/64 - 1 of every sequence, all layers,
+ * then sealed[b] = seq_len[b]/64.  The scale of a tile (page, head, K or V) is the smallest power of two 2^e, -60 <= e <= 60, with
+ * max |x| <= 448 * 2^e; values are x / 2^e rounded to the nearest e4m3 number, ties to even.  Values are expected to be finite: beyond 448 * 2^60 they
+ * are cut off there, NaN stays NaN.  A sequence with seq_len, sealed or page ids out of range is reported in `status` and sealed[b] stays (pages of
+ * the 8-bit cache that it names may have been written).  Two launches. */
+int sage_seal_kv(const void *k_pool, const void *v_pool, int64_t layer_stride_elems, int n_layers, int n_pages,
+                 const int32_t *page_table, int max_pages_per_seq, const int32_t *seq_len,
+                 const sage_sealed_cache *cache, int32_t *sealed, int batch,
+                 int n_kv_heads, int head_dim, int page_size, int32_t *status, void *stream);
+
+/* Tree attention over a cache whose first sealed[b] pages are sealed (0 <= sealed[b] <= L_b / 64) and the rest, with the tree's rows, bf16:
+ * as sage_tree_attention in everything else.  Sealed keys and values enter the products as the 8-bit numbers that they are, queries as the
+ * sum of two e4m3 numbers (off by 2^-17 of the row's largest element at most) and probabilities as the sum of an e4m3 and an
+ * e5m2 number (off by 2^-7 of their value, or 2^-23 of a value near the row's largest).  Values of a sequence whose scales differ by more than about
+ * 2^20 lose precision relative to the largest.  ws: sage_tree_attention_sealed_workspace_size(...)
+ * bytes, for the same sizes.  One or two launches. */
+int sage_tree_attention_sealed(const void *q, const void *k_pool, const void *v_pool,
+                               int64_t layer_stride_elems, int n_layers, int n_pages,
+                               const int32_t *page_table, int max_pages_per_seq,
+                               const sage_sealed_cache *cache, const int32_t *sealed, const int32_t *seq_len,
+                               const int32_t *parent, const int32_t *node_offsets, int batch, int sum_nodes,
+                               int n_q_heads, int n_kv_heads, int head_dim, int page_size, float sm_scale,
+                               void *out, void *ws, size_t ws_bytes, int32_t *status, void *stream);
+size_t sage_tree_attention_sealed_workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads,
+                                                 int head_dim, int max_pages_per_seq);
 
 const char *sage_status_string(int code);
 

@@ -18,6 +18,10 @@ _BINDING_NAMES = (
     "SageHistoryPolicy", "sage_tree_attention", "sage_tree_attention_workspace_size",
     "sage_accept", "sage_compact_kv", "sage_debug_attention_waits", "sage_debug_attention_schedule",
     "sage_debug_attention_plan",
+    "sage_rope_append", "make_rope_policy", "SageRopePolicy", "SageRopeRows",
+    "sage_seal_kv", "new_sealed_cache", "SageSealedCache",
+    "sage_tree_attention_sealed", "sage_tree_attention_sealed_workspace_size",
+    "sage_tree_attention_window", "sage_tree_attention_window_workspace_size",
     "SAGE_OK", "SAGE_ERR_INVALID_ARG", "SAGE_ERR_UNSUPPORTED", "SAGE_ERR_WORKSPACE", "SAGE_ERR_CUDA",
     "SAGE_ERR_TOO_LARGE", "SAGE_STATIC_SCRATCH_BYTES",
     "SAGE_STATUS_BAD_TREE", "SAGE_STATUS_BAD_PAGE", "SAGE_STATUS_TIMEOUT", "SAGE_STATUS_BAD_PATH",

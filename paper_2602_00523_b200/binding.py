@@ -51,6 +51,24 @@ class SageHistoryPolicy(ctypes.Structure):
                 ("d_lo", ctypes.c_float), ("d_hi", ctypes.c_float)]
 
 
+class SageRopePolicy(ctypes.Structure):
+    """Mirror of ``sage_rope_policy``."""
+    _fields_ = [("inv_freq", ctypes.c_double * 64), ("axis", ctypes.c_uint8 * 64), ("scale", ctypes.c_float)]
+
+
+class SageRopeRows(ctypes.Structure):
+    """Mirror of ``sage_rope_rows``."""
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + [
+        (f"{t}_{d}_stride", ctypes.c_int64) for t in "qkv" for d in ("layer", "token")]
+
+
+class SageSealedCache(ctypes.Structure):
+    """Mirror of ``sage_sealed_cache``."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("k_exp", ctypes.c_void_p),
+                ("v_exp", ctypes.c_void_p), ("n_pages", ctypes.c_int), ("page_table", ctypes.c_void_p),
+                ("max_pages_per_seq", ctypes.c_int)]
+
+
 class SageError(RuntimeError):
     def __init__(self, code: int, where: str):
         self.code = code
@@ -94,6 +112,21 @@ _lib.sage_accept.restype = _i
 _lib.sage_accept.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp]
 _lib.sage_compact_kv.restype = _i
 _lib.sage_compact_kv.argtypes = [_vp, _vp, _i64, _i, _i, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _i, _vp, _vp]
+_lib.sage_rope_append.restype = _i
+_lib.sage_rope_append.argtypes = [ctypes.POINTER(SageRopeRows), ctypes.POINTER(SageRopePolicy), _i, _i, _i, _i, _i, _vp, _vp, _vp,
+                                  _vp, _vp, _vp, _i64, _i, _i, _vp, _i, _vp, _vp, _i, _vp, _vp]
+_lib.sage_seal_kv.restype = _i
+_lib.sage_seal_kv.argtypes = [_vp, _vp, _i64, _i, _i, _vp, _i, _vp, ctypes.POINTER(SageSealedCache), _vp, _i, _i, _i, _i, _vp, _vp]
+_lib.sage_tree_attention_window.restype = _i
+_lib.sage_tree_attention_window.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _vp, _i, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _f, _i, _i,
+                                            _vp, _vp, _sz, _vp, _vp]
+_lib.sage_tree_attention_window_workspace_size.restype = _sz
+_lib.sage_tree_attention_window_workspace_size.argtypes = [_i] * 9
+_lib.sage_tree_attention_sealed.restype = _i
+_lib.sage_tree_attention_sealed.argtypes = [_vp, _vp, _vp, _i64, _i, _i, _vp, _i, ctypes.POINTER(SageSealedCache), _vp, _vp, _vp, _vp,
+                                            _i, _i, _i, _i, _i, _i, _f, _vp, _vp, _sz, _vp, _vp]
+_lib.sage_tree_attention_sealed_workspace_size.restype = _sz
+_lib.sage_tree_attention_sealed_workspace_size.argtypes = [_i] * 7
 _lib.sage_debug_attention_waits.restype = None
 _lib.sage_debug_attention_waits.argtypes = [ctypes.c_longlong, _i]
 _lib.sage_debug_attention_schedule.restype = None
@@ -255,6 +288,118 @@ def sage_tree_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Ten
         ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
     _check(_native.tree_attention(q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, out, ws, status, stream),
            "sage_tree_attention")
+    return out
+
+
+def sage_tree_attention_window_workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, head_dim, max_pages, window,
+                                              sink) -> int:
+    most = 2 ** 31 - 1
+    return int(_lib.sage_tree_attention_window_workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, head_dim, max_pages,
+                                                              min(int(window), most), min(int(sink), most)))
+
+
+def sage_tree_attention_window(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor,
+                               seq_len: torch.Tensor, parent: torch.Tensor, node_offsets: torch.Tensor, sm_scale: float,
+                               window: int, sink: int = 0, *, out=None, ws=None, status=None, stream=None) -> torch.Tensor:
+    """sage_tree_attention of rows that see the last ``window`` positions and the first ``sink`` ones only; shapes as there."""
+    if out is None:
+        out = torch.empty_like(q)
+    if ws is None:
+        n_layers, sum_nodes, Hq, d = q.shape
+        need = sage_tree_attention_window_workspace_size(n_layers, page_table.shape[0], sum_nodes, Hq, k_pool.shape[2], d,
+                                                         page_table.shape[1], window, sink)
+        ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+    _check(_native.tree_attention_window(q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, window, sink, out, ws,
+                                         status, stream), "sage_tree_attention_window")
+    return out
+
+
+def make_rope_policy(base: float = 10000.0, sections=(64, 0, 0), *, interleaved: bool = False, scale: float = 1.0,
+                     inv_freq=None) -> SageRopePolicy:
+    """Frequencies base ** (-i / 64), i < 64 (or 64 given ones), and the axis of each: ``sections`` frequencies for time, height
+    and width one after the other, or, ``interleaved``, in turn (time, height, width, time, ...) as long as an axis has some
+    left.  The default is the ordinary one-axis rotation; ``scale`` multiplies the turned rows."""
+    sections = [int(n) for n in sections]
+    if len(sections) != 3 or min(sections) < 0 or sum(sections) != 64:
+        raise ValueError("sections: three counts that sum to 64")
+    if interleaved:
+        left, axis = list(sections), []
+        while len(axis) < 64:
+            for a in range(3):
+                if left[a]:
+                    left[a] -= 1
+                    axis.append(a)
+    else:
+        axis = [a for a, n in enumerate(sections) for _ in range(n)]
+    freq = [float(base) ** (-i / 64.0) for i in range(64)] if inv_freq is None else [float(f) for f in inv_freq]
+    if len(freq) != 64:
+        raise ValueError("inv_freq: 64 values")
+    p = SageRopePolicy()
+    for i in range(64):
+        p.inv_freq[i], p.axis[i] = freq[i], axis[i]
+    p.scale = float(scale)
+    return p
+
+
+def sage_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, policy: SageRopePolicy, k_pool: torch.Tensor,
+                     v_pool: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor, node_offsets: torch.Tensor, *, pos=None,
+                     parent=None, next_pos=None, out=None, status=None, stream=None) -> torch.Tensor:
+    """q bf16 [layers, tokens, Hq, d], k and v [layers, tokens, Hkv, d]: the heads of a token side by side, tokens and layers at
+    any distance (parts of a fused projection's rows).  Returns the turned queries (``out``, contiguous) and writes turned keys, and
+    values, behind each sequence's prefix into the pools.  Positions: ``pos`` int32 [3, tokens], or ``parent`` and ``next_pos`` [B]."""
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    _check(_native.rope_append(q, k, v, policy, k_pool, v_pool, page_table, seq_len, node_offsets, pos, parent, next_pos, out, status,
+                               stream), "sage_rope_append")
+    return out
+
+
+def new_sealed_cache(n_layers: int, n_pages: int, n_kv_heads: int, page_table: torch.Tensor, *, page_size: int = 64,
+                     head_dim: int = 128) -> Dict[str, torch.Tensor]:
+    """An empty 8-bit cache for pages that are full: k, v (e4m3 [layers, pages, Hkv, P, d]), k_exp, v_exp (bytes [layers, pages,
+    Hkv]) and the page table (int32 [B, max_pages], ids of these pools) that it goes by."""
+    dev = page_table.device
+    shape = (n_layers, n_pages, n_kv_heads)
+    cache = {"page_table": page_table}
+    for name in ("k", "v"):
+        cache[name] = torch.zeros(shape + (page_size, head_dim), dtype=torch.uint8, device=dev).view(torch.float8_e4m3fn)
+        cache[name + "_exp"] = torch.full(shape, 127, dtype=torch.uint8, device=dev)
+    return cache
+
+
+def _sealed(code, where: str):
+    if code is None:
+        raise KeyError("cache needs k, v, k_exp, v_exp and page_table")
+    _check(code, where)
+
+
+def sage_seal_kv(k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor, seq_len: torch.Tensor, sealed: torch.Tensor,
+                 cache: Dict[str, torch.Tensor], *, status=None, stream=None) -> Dict[str, torch.Tensor]:
+    """Full pages of the prefix that are not sealed yet move into ``cache`` (see new_sealed_cache); ``sealed`` int32 [B], in
+    place: the number of each sequence's first pages that are held there."""
+    _sealed(_native.seal_kv(k_pool, v_pool, page_table, seq_len, sealed, cache, status, stream), "sage_seal_kv")
+    return cache
+
+
+def sage_tree_attention_sealed_workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, head_dim, max_pages) -> int:
+    return int(_lib.sage_tree_attention_sealed_workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, head_dim, max_pages))
+
+
+def sage_tree_attention_sealed(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Tensor, page_table: torch.Tensor,
+                               cache: Dict[str, torch.Tensor], sealed: torch.Tensor, seq_len: torch.Tensor, parent: torch.Tensor,
+                               node_offsets: torch.Tensor, sm_scale: float, *, out=None, ws=None, status=None,
+                               stream=None) -> torch.Tensor:
+    """sage_tree_attention over a cache whose first ``sealed[b]`` pages lie in ``cache`` and whose others, with the tree's rows, lie
+    in the bf16 pools; shapes as there."""
+    if out is None:
+        out = torch.empty_like(q)
+    if ws is None:
+        n_layers, sum_nodes, Hq, d = q.shape
+        need = sage_tree_attention_sealed_workspace_size(n_layers, page_table.shape[0], sum_nodes, Hq, k_pool.shape[2], d,
+                                                         page_table.shape[1])
+        ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+    _sealed(_native.tree_attention_sealed(q, k_pool, v_pool, page_table, cache, sealed, seq_len, parent, node_offsets, sm_scale, out, ws,
+                                          status, stream), "sage_tree_attention_sealed")
     return out
 
 

@@ -12,12 +12,13 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libsage.so")
 NATIVE_PATH = os.path.join(PKG_DIR, "_native" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
-SOURCES = ["tree_ops.cu", "logits_stats.cu", "tree_attention.cu", "tree_attention_rows.cu", "tree_attention_alt.cu", "tree_attention_split.cu"]
+SOURCES = ["tree_ops.cu", "logits_stats.cu", "tree_attention.cu", "tree_attention_rows.cu", "tree_attention_alt.cu", "tree_attention_split.cu",
+           "cache/rope_append.cu", "cache/seal_kv.cu", "cache/tree_attention_paged.cu"]
 NATIVE_SOURCE = "binding.cpp"
 
 
 def _newest_source_mtime() -> float:
-    paths = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(ROOT, "include", "sage.h")]
+    paths = [os.path.join(d, f) for d, _, files in os.walk(CSRC) for f in files] + [os.path.join(ROOT, "include", "sage.h")]
     return max(os.path.getmtime(p) for p in paths)
 
 

@@ -6,6 +6,7 @@
 // Every function takes its arguments by position and returns the entry point's code; None means that `out` lacks
 // a tensor (the Python wrapper then allocates and calls again).  The GIL is released around the C call.
 #include <Python.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -70,7 +71,7 @@ T structure(PyObject* o) {
 struct Names {
     PyObject *topk_idx, *topk_logprob, *entropy_full, *entropy_topk, *alpha, *lse, *draft_token, *template_id, *depth_cont,
         *width_cont, *next_parent, *next_rank, *next_node_offsets, *parent, *rank, *depth, *token, *cum_logprob, *n_nodes,
-        *frontier_begin, *path, *path_len, *bonus_token;
+        *frontier_begin, *path, *path_len, *bonus_token, *k, *v, *k_exp, *v_exp, *page_table;
 } N;
 
 struct Missing {};                                  // `out` lacks an entry
@@ -314,9 +315,229 @@ PyObject* compact_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// The calls around the paged cache hold their tensors to one device, run on it whichever is the current one (without a stream of
+// the caller's: on its current stream), and check types and shapes: what the C entry points are given are sizes of one tensor for all.
+class OneDevice {
+public:
+    // The tensor, checked; its size along each dimension where `sizes` names one (-1: any).
+    const at::Tensor& need(PyObject* o, const char* name, std::initializer_list<at::ScalarType> types, std::initializer_list<int64_t> sizes,
+                           bool contiguous = true) {
+        const at::Tensor& t = tensor(o);
+        if (!t.is_cuda()) fail(PyExc_ValueError, "device tensors only");
+        if (device_ < 0) device_ = t.get_device();
+        if (t.get_device() != device_) bad(name, "on another device than the others");
+        bool type = false;
+        for (at::ScalarType k : types) type |= t.scalar_type() == k;
+        if (!type) bad(name, "of another element type than documented");
+        if (t.dim() != static_cast<int64_t>(sizes.size())) bad(name, "of another number of dimensions than documented");
+        int64_t i = 0;
+        for (int64_t n : sizes) {
+            if (n >= 0 && t.size(i) != n) bad(name, "of another size than the others say");
+            ++i;
+        }
+        if (contiguous && !t.is_contiguous()) bad(name, "not contiguous");
+        return t;
+    }
+    template <typename T = void>
+    T* at(PyObject* o, const char* name, std::initializer_list<at::ScalarType> types, std::initializer_list<int64_t> sizes) {
+        return static_cast<T*>(need(o, name, types, sizes).data_ptr());
+    }
+    int32_t* i32(PyObject* o, const char* name, std::initializer_list<int64_t> sizes) { return at<int32_t>(o, name, {at::kInt}, sizes); }
+    int32_t* status(PyObject* o) { return o == Py_None ? nullptr : i32(o, "status", {1}); }
+    int device() const { return device_; }
+
+private:
+    [[noreturn]] static void bad(const char* name, const char* what) {
+        PyErr_Format(PyExc_ValueError, "%s: %s", name, what);
+        throw Failed{};
+    }
+    int device_ = -1;
+};
+// Makes a device current, and says which stream a call goes to.
+struct On {
+    c10::cuda::CUDAGuard guard;
+    explicit On(const OneDevice& d) : guard(static_cast<c10::DeviceIndex>(d.device())) {}
+};
+struct Cache16 {
+    void *k, *v;
+    int64_t layer_stride;
+    int layers, pages, kv_heads;
+};
+// The bf16 pools: one shape, pages of a layer without gaps, layers at one distance.
+Cache16 cache16(OneDevice& d, PyObject* ko, PyObject* vo, int64_t layers) {
+    const at::Tensor& k = d.need(ko, "k_pool", {at::kBFloat16}, {layers, -1, -1, -1, -1}, false);
+    const at::Tensor& v = d.need(vo, "v_pool", {at::kBFloat16}, {layers, k.size(1), k.size(2), k.size(3), k.size(4)}, false);
+    const int64_t in_layer = k.size(1) * k.size(2) * k.size(3) * k.size(4);
+    for (const at::Tensor* t : {&k, &v})
+        if (layers > 0 && !t->select(0, 0).is_contiguous()) fail(PyExc_ValueError, "pools: a layer's pages lie without gaps");
+    if (layers > 1 && k.stride(0) != v.stride(0)) fail(PyExc_ValueError, "pools: layers at the same distance in both");
+    return {k.data_ptr(), v.data_ptr(), layers > 1 ? k.stride(0) : in_layer, size32(layers), size32(k.size(1)), size32(k.size(2))};
+}
+// A mapping with k, v (e4m3 or bytes), k_exp, v_exp and page_table.
+sage_sealed_cache sealed_cache(OneDevice& d, PyObject* o, int64_t layers, int64_t kv_heads, int64_t page, int64_t dim, int64_t batch) {
+    Tensors c(o);
+    const auto e4m3 = {at::kFloat8_e4m3fn, at::kByte};
+    PyObject *ko = c[N.k], *vo = c[N.v], *ke = c[N.k_exp], *ve = c[N.v_exp], *po = c[N.page_table];
+    const at::Tensor& k = d.need(ko, "cache k", e4m3, {layers, -1, kv_heads, page, dim}, false);
+    const at::Tensor& v = d.need(vo, "cache v", e4m3, {layers, k.size(1), kv_heads, page, dim}, false);
+    for (const at::Tensor* t : {&k, &v})
+        if (layers > 0 && !t->select(0, 0).is_contiguous()) fail(PyExc_ValueError, "cache: a layer's pages lie without gaps");
+    if (layers > 1 && k.stride(0) != v.stride(0)) fail(PyExc_ValueError, "cache: layers at the same distance in both");
+    sage_sealed_cache s{};
+    s.k = k.data_ptr();
+    s.v = v.data_ptr();
+    s.layer_stride = layers > 1 ? k.stride(0) : k.size(1) * kv_heads * page * dim;
+    s.k_exp = d.at<uint8_t>(ke, "cache k_exp", {at::kByte}, {layers, k.size(1), kv_heads});
+    s.v_exp = d.at<uint8_t>(ve, "cache v_exp", {at::kByte}, {layers, k.size(1), kv_heads});
+    s.n_pages = size32(k.size(1));
+    const at::Tensor& t = d.need(po, "cache page_table", {at::kInt}, {batch, -1});
+    s.page_table = static_cast<const int32_t*>(t.data_ptr());
+    s.max_pages_per_seq = size32(t.size(1));
+    return s;
+}
+
+// q, k, v, policy, k_pool, v_pool, page_table, seq_len, node_offsets, pos, parent, next_pos, out, status, stream
+PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 15, [&]() -> int {
+        OneDevice d;
+        const at::Tensor& q = d.need(a[0], "q", {at::kBFloat16}, {-1, -1, -1, -1}, false);
+        const int64_t layers = q.size(0), tokens = q.size(1), dim = q.size(3);
+        const Cache16 c = cache16(d, a[4], a[5], layers);
+        const at::Tensor& pool = tensor(a[4]);
+        const at::Tensor& k = d.need(a[1], "k", {at::kBFloat16}, {layers, tokens, c.kv_heads, dim}, false);
+        const at::Tensor& v = d.need(a[2], "v", {at::kBFloat16}, {layers, tokens, c.kv_heads, dim}, false);
+        if (pool.size(4) != dim) fail(PyExc_ValueError, "q, k, v and the pools have one head dimension");
+        sage_rope_rows r{};
+        r.q = q.data_ptr();
+        r.k = k.data_ptr();
+        r.v = v.data_ptr();
+        int64_t* strides[3][2] = {{&r.q_layer_stride, &r.q_token_stride}, {&r.k_layer_stride, &r.k_token_stride}, {&r.v_layer_stride, &r.v_token_stride}};
+        const at::Tensor* rows[3] = {&q, &k, &v};
+        for (int i = 0; i < 3; ++i) {
+            const at::Tensor& t = *rows[i];
+            if (t.numel() > 0 && (t.stride(3) != 1 || (t.size(2) > 1 && t.stride(2) != dim)))
+                fail(PyExc_ValueError, "q, k, v: the heads of a token lie side by side");
+            *strides[i][0] = layers > 1 ? t.stride(0) : 0;
+            *strides[i][1] = tokens > 1 ? t.stride(1) : 0;
+        }
+        const sage_rope_policy pol = structure<sage_rope_policy>(a[3]);
+        const at::Tensor& pt = d.need(a[6], "page_table", {at::kInt}, {-1, -1});
+        const int64_t batch = pt.size(0);
+        const int32_t *len = d.i32(a[7], "seq_len", {batch}), *offs = d.i32(a[8], "node_offsets", {batch + 1});
+        const int32_t* pos = a[9] == Py_None ? nullptr : d.i32(a[9], "pos", {3, tokens});
+        const int32_t* parent = a[10] == Py_None ? nullptr : d.i32(a[10], "parent", {tokens});
+        const int32_t* next = a[11] == Py_None ? nullptr : d.i32(a[11], "next_pos", {batch});
+        void* out = d.at(a[12], "out", {at::kBFloat16}, {layers, tokens, q.size(2), dim});
+        int32_t* status = d.status(a[13]);
+        const On on(d);
+        void* stream = stream_of(a[14]);
+        if (layers == 0 || tokens == 0) return SAGE_OK;
+        const int nl = size32(layers), nt = size32(tokens), hq = size32(q.size(2)), hd = size32(dim), page = size32(pool.size(3)),
+                  width = size32(pt.size(1)), nb = size32(batch);
+        const int32_t* table = static_cast<const int32_t*>(pt.data_ptr());
+        return without_gil([&] {
+            return sage_rope_append(&r, &pol, nl, nt, hq, c.kv_heads, hd, pos, parent, next, out, c.k, c.v, c.layer_stride, c.pages, page, table,
+                                    width, len, offs, nb, status, stream);
+        });
+    });
+}
+
+// k_pool, v_pool, page_table, seq_len, sealed, cache, status, stream
+PyObject* seal_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&]() -> int {
+        OneDevice d;
+        const at::Tensor& pool = tensor(a[0]);
+        if (pool.dim() != 5) fail(PyExc_ValueError, "pools: [layers, pages, kv heads, page, head dim]");
+        const Cache16 c = cache16(d, a[0], a[1], pool.size(0));
+        const at::Tensor& pt = d.need(a[2], "page_table", {at::kInt}, {-1, -1});
+        const int64_t batch = pt.size(0);
+        const int32_t* len = d.i32(a[3], "seq_len", {batch});
+        int32_t* sealed = d.i32(a[4], "sealed", {batch});
+        const sage_sealed_cache s8 = sealed_cache(d, a[5], c.layers, c.kv_heads, pool.size(3), pool.size(4), batch);
+        int32_t* status = d.status(a[6]);
+        const On on(d);
+        void* stream = stream_of(a[7]);
+        const int32_t* table = static_cast<const int32_t*>(pt.data_ptr());
+        const int width = size32(pt.size(1)), nb = size32(batch), page = size32(pool.size(3)), dim = size32(pool.size(4));
+        return without_gil([&] {
+            return sage_seal_kv(c.k, c.v, c.layer_stride, c.layers, c.pages, table, width, len, &s8, sealed, nb, c.kv_heads, dim, page, status,
+                                stream);
+        });
+    });
+}
+
+// What both forms of attention take, checked.
+struct Attention {
+    OneDevice d;
+    Cache16 c;
+    const void* q;
+    void *out, *ws;
+    size_t ws_bytes;
+    const int32_t *table, *len, *parent, *offs;
+    int32_t* status;
+    int nodes, heads, dim, page, batch, width;
+    float scale;
+    // q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, out, ws, status
+    Attention(PyObject* qo, PyObject* ko, PyObject* vo, PyObject* po, PyObject* lo, PyObject* to, PyObject* no, PyObject* so, PyObject* oo,
+              PyObject* wo, PyObject* st) {
+        const at::Tensor& qt = d.need(qo, "q", {at::kBFloat16}, {-1, -1, -1, -1});
+        c = cache16(d, ko, vo, qt.size(0));
+        const at::Tensor& pool = tensor(ko);
+        if (pool.size(4) != qt.size(3)) fail(PyExc_ValueError, "q and the pools have one head dimension");
+        const at::Tensor& pt = d.need(po, "page_table", {at::kInt}, {-1, -1});
+        const int64_t b = pt.size(0), n = qt.size(1);
+        len = d.i32(lo, "seq_len", {b});
+        parent = d.i32(to, "parent", {n});
+        offs = d.i32(no, "node_offsets", {b + 1});
+        out = d.at(oo, "out", {at::kBFloat16}, {qt.size(0), n, qt.size(2), qt.size(3)});
+        const at::Tensor& w = d.need(wo, "ws", {at::kByte}, {-1});
+        ws = w.data_ptr();
+        ws_bytes = static_cast<size_t>(w.numel());
+        status = d.status(st);
+        const double s = PyFloat_AsDouble(so);
+        if (s == -1.0 && PyErr_Occurred()) throw Failed{};
+        scale = static_cast<float>(s);
+        q = qt.data_ptr();
+        table = static_cast<const int32_t*>(pt.data_ptr());
+        nodes = size32(n); heads = size32(qt.size(2)); dim = size32(qt.size(3)); page = size32(pool.size(3)); batch = size32(b); width = size32(pt.size(1));
+    }
+};
+
+// q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, window, sink, out, ws, status, stream
+PyObject* tree_attention_window(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 14, [&]() -> int {
+        const Attention t(a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[10], a[11], a[12]);
+        const int window = integer(a[8]), sink = integer(a[9]);
+        const On on(t.d);
+        void* stream = stream_of(a[13]);
+        return without_gil([&] {
+            return sage_tree_attention_window(t.q, t.c.k, t.c.v, t.c.layer_stride, t.c.layers, t.c.pages, t.table, t.width, t.len, t.parent, t.offs,
+                                              t.batch, t.nodes, t.heads, t.c.kv_heads, t.dim, t.page, t.scale, window, sink, t.out, t.ws, t.ws_bytes,
+                                              t.status, stream);
+        });
+    });
+}
+
+// q, k_pool, v_pool, page_table, cache, sealed, seq_len, parent, node_offsets, sm_scale, out, ws, status, stream
+PyObject* tree_attention_sealed(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 14, [&]() -> int {
+        Attention t(a[0], a[1], a[2], a[3], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
+        const int32_t* sealed = t.d.i32(a[5], "sealed", {t.batch});
+        const sage_sealed_cache s8 = sealed_cache(t.d, a[4], t.c.layers, t.c.kv_heads, t.page, t.dim, t.batch);
+        const On on(t.d);
+        void* stream = stream_of(a[13]);
+        return without_gil([&] {
+            return sage_tree_attention_sealed(t.q, t.c.k, t.c.v, t.c.layer_stride, t.c.layers, t.c.pages, t.table, t.width, &s8, sealed, t.len,
+                                              t.parent, t.offs, t.batch, t.nodes, t.heads, t.c.kv_heads, t.dim, t.page, t.scale, t.out, t.ws,
+                                              t.ws_bytes, t.status, stream);
+        });
+    });
+}
+
 #define ENTRY(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {ENTRY(expand_topk), ENTRY(select_tree), ENTRY(grow_tree), ENTRY(update_history),
-                          ENTRY(build_ancestor_mask), ENTRY(tree_attention), ENTRY(accept), ENTRY(compact_kv),
+                          ENTRY(build_ancestor_mask), ENTRY(tree_attention), ENTRY(accept), ENTRY(compact_kv), ENTRY(rope_append), ENTRY(seal_kv),
+                          ENTRY(tree_attention_window), ENTRY(tree_attention_sealed),
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Marshalling of libsage.so's calls.", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};
@@ -329,6 +550,7 @@ PyMODINIT_FUNC PyInit__native() {
     NAME(template_id); NAME(depth_cont); NAME(width_cont); NAME(next_parent); NAME(next_rank); NAME(next_node_offsets);
     NAME(parent); NAME(rank); NAME(depth); NAME(token); NAME(cum_logprob); NAME(n_nodes); NAME(frontier_begin);
     NAME(path); NAME(path_len); NAME(bonus_token);
+    NAME(k); NAME(v); NAME(k_exp); NAME(v_exp); NAME(page_table);
 #undef NAME
     return PyModule_Create(&kModule);
 }

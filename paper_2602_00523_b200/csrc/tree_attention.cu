@@ -6,6 +6,7 @@
 
 #include <mutex>
 
+#include "cache/paged.cuh"
 #include "sage_common.cuh"
 
 namespace sage {
@@ -60,7 +61,7 @@ static bool cached_map(CUtensorMap* out, const MapKey& key, Make make) {
 }
 
 // Pool viewed as [layer][page*Hkv + head][slot][d]; one box = one 64-wide d-half of one (page, head).
-static bool make_pool_map(CUtensorMap* map, const void* pool, int n_layers, int n_pages, int n_kv_heads,
+bool make_pool_map(CUtensorMap* map, const void* pool, int n_layers, int n_pages, int n_kv_heads,
                           int64_t layer_stride_elems) {
     const MapKey key{pool, n_layers, n_pages, n_kv_heads, layer_stride_elems, 0};
     return cached_map(map, key, [&](CUtensorMap* m) {
@@ -79,9 +80,26 @@ static bool make_pool_map(CUtensorMap* map, const void* pool, int n_layers, int 
     });
 }
 
+// The same of a pool of sealed pages: e4m3 rows of 128 bytes, one box a whole (page, head).
+bool make_sealed_map(CUtensorMap* map, const void* pool, int n_layers, int n_pages, int n_kv_heads, int64_t layer_stride_bytes) {
+    const MapKey key{pool, n_layers, n_pages, n_kv_heads, layer_stride_bytes, 2};
+    return cached_map(map, key, [&](CUtensorMap* m) {
+        EncodeTiledFn fn = encode_fn();
+        if (!fn) return false;
+        const cuuint64_t page_head_bytes = (cuuint64_t)kPageSize * kHeadDim;
+        cuuint64_t dims[4] = {(cuuint64_t)kHeadDim, (cuuint64_t)kPageSize, (cuuint64_t)n_pages * n_kv_heads, (cuuint64_t)n_layers};
+        cuuint64_t layer_bytes = n_layers > 1 ? (cuuint64_t)layer_stride_bytes : dims[2] * page_head_bytes;
+        cuuint64_t strides[3] = {(cuuint64_t)kHeadDim, page_head_bytes, layer_bytes};
+        cuuint32_t box[4] = {(cuuint32_t)kHeadDim, (cuuint32_t)kPageSize, 1, 1};
+        cuuint32_t estr[4] = {1, 1, 1, 1};
+        return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(pool), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    });
+}
+
 // Queries viewed as [layer][node][kv head][head in group][d]; one box = one 64-wide d-half of the
 // 128 query rows (128/G nodes x G heads) of a row tile.  Nodes past sum_nodes read as zero.
-static bool make_q_map(CUtensorMap* map, const void* q, int n_layers, int sum_nodes, int n_kv_heads, int G) {
+bool make_q_map(CUtensorMap* map, const void* q, int n_layers, int sum_nodes, int n_kv_heads, int G) {
     const MapKey key{q, n_layers, sum_nodes, n_kv_heads, G, 1};
     return cached_map(map, key, [&](CUtensorMap* m) {
         EncodeTiledFn fn = encode_fn();
@@ -99,7 +117,7 @@ static bool make_q_map(CUtensorMap* map, const void* q, int n_layers, int sum_no
 }
 
 // One resident CTA per SM (148 when no device can be asked, e.g. a size query on a host without a GPU).
-static int resident_ctas() {
+int resident_ctas() {
     static int cached[64] = {};
     int dev = 0;
     if (!succeeded(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return 148;
@@ -112,6 +130,8 @@ static int resident_ctas() {
 }
 static long long g_wait_cycles = kWaitCyclesDefault;
 static int g_producer_off = 0;
+long long attention_wait_cycles() { return g_wait_cycles; }
+int attention_producer_off() { return g_producer_off; }
 static int g_schedule = 0;     // 0: chosen per launch, 2: split, else streaming
 
 // The split schedule (tree_attention_split.cu).

@@ -1,5 +1,5 @@
 // What the operators around the paged cache share: the tensor maps and settings of the attention entry points
-// (tree_attention.cu), the merge of context slices (tree_attention_split.cu), and the parameters of the paged kernel.
+// (tree_attention.cu), and the parameters of the paged kernel.
 #pragma once
 
 #include <cuda.h>
@@ -16,20 +16,12 @@ int resident_ctas();
 long long attention_wait_cycles();
 int attention_producer_off();
 
-namespace split {
-constexpr int kMaxSplits = 32;
-// Merges partial results [layer][slice][32 column quads][sum_nodes*Hq rows] (and their (reference, sum)) into out.
-// overlap: brought up while the kernel in front still runs.
-int launch_merge(int n_layers, const int32_t* node_offsets, int batch, int sum_nodes, int n_q_heads, int n_splits, const void* part_o,
-                 const void* part_ml, void* out, bool overlap, cudaStream_t stream);
-}  // namespace split
-
 namespace paged {
 
 struct Params {
     __nv_bfloat16* out;
-    float4* part_o;    // [layer][slice][32 column quads][sum_nodes*Hq rows]   unnormalised
-    float2* part_ml;   // [layer][slice][sum_nodes*Hq rows]                    (reference in log2 units, sum)
+    float4* part_o;    // [item behind the whole ones][slice][32 column quads][row_tiles*128 rows]   unnormalised
+    float2* part_ml;   // [item behind the whole ones][slice][row_tiles*128 rows]                    (reference in log2 units, sum)
     const int32_t* page_table;
     const int32_t* page_table8;     // of the sealed pages
     const int32_t* sealed;          // sealed pages of each sequence; null: the cache is bf16 throughout
@@ -41,7 +33,8 @@ struct Params {
     int32_t* status;
     int n_layers, batch, sum_nodes, n_pages, max_pages, n_pages8, max_pages8;
     int Hq, Hkv, G, g_shift;        // G = 1 << g_shift query heads per KV head
-    int n_splits, row_tiles;        // context slices; 128-row tiles of the largest possible tree
+    int n_whole, n_splits;          // items that are not cut, context slices of the others
+    int row_tiles;                  // 128-row tiles of the largest possible tree
     int window, sink;
     float scale_log2;               // sm_scale * log2(e)
     long long wait_cycles;          // budget of every on-device wait

@@ -33,7 +33,8 @@ using namespace stream;
 constexpr int kSlots = 5;                                   // ring of 16 KB slots
 constexpr int kSlotBytes = kPageSize * kHeadDim * 2;        // a bf16 K or V page of a head, or both of a sealed one
 constexpr int kSealedBytes = kPageSize * kHeadDim;          // a sealed K or V page of a head
-constexpr int kThreads = 192;                               // a softmax warpgroup, the TMA warp, the MMA warp
+constexpr int kMostSplits = 32;                             // slices of an item
+constexpr int kThreads = 256;                               // a softmax warpgroup; the TMA warp, the MMA warp and two idle ones
 constexpr int kTmemColumns = 256;                           // S 2 x 64, O 128
 constexpr uint32_t kIdescPage = idesc_f16(kPageSize);       // S = Q K^T, bf16
 // kind::f8f6f4: D fp32, M = 128; types of A: 0 e4m3, 1 e5m2; B e4m3
@@ -41,9 +42,14 @@ constexpr uint32_t idesc_f8(uint32_t n, uint32_t a_type) { return (1u << 4) | (a
 constexpr uint32_t kIdescSealedQK = idesc_f8(kPageSize, 0);
 constexpr uint32_t kIdescSealedPVHigh = idesc_f8(kHeadDim, 0) | (1u << 16);     // B (= V) MN-major
 constexpr uint32_t kIdescSealedPVLow = idesc_f8(kHeadDim, 1) | (1u << 16);
-// Probabilities are taken against a reference 2^kHeadroom below the maximum that set it, and may reach 448 = 2^8.807 (e4m3's
-// largest): a row's maximum may grow by 2.8 (in log2; 1.9 in the scores) before the accumulator is scaled again.
-constexpr float kHeadroom = 6.f, kMostLog2 = 8.807f;
+// Probabilities are taken against a reference 2^headroom below the maximum that set it, and may reach 448 = 2^8.807 (e4m3's largest): a
+// row's maximum may grow by 2^(8.8 - headroom) before the accumulator is scaled again.  At first, when most of the growth is still to come, a headroom
+// of 3 (a page's maximum may lie 4 below the row's in the scores), later 5.  With 6 throughout, eleven of 65 pages of 16k normally distributed keys
+// had to move some row of their warp, now three.
+constexpr float kHeadroomFirst = 3.f, kHeadroom = 5.f, kMostLog2 = 8.807f;
+constexpr int kEmuPairs = 0;
+constexpr uint32_t kMostF16 = 0x5f00;       // 448 as fp16 bits
+constexpr float kMostSum = 32.f * kMaxSum;  // bf16 pages: what the probabilities of a page may sum to (kMaxSum is against the maximum itself)
 // Exponents of sealed scales (sage_seal_kv writes no others; a byte outside is read as the nearest).
 constexpr int kExpLo = 127 - 60, kExpHi = 127 + 60;
 
@@ -64,6 +70,17 @@ struct __align__(8) Shared {
 constexpr int kSmemBytes = kQTileBytes + kSlots * kSlotBytes + 1024;
 static_assert(sizeof(Shared) <= 1024 && 2 * (kSmemBytes + 1024) <= 233472, "two blocks have to fit on an SM");
 
+// mbar_wait_warp with its loop apart: a dozen waits in line are a fifth of the kernel's code, and what the warps of an SM run at the same time has to
+// fit its instruction caches.
+static __device__ __noinline__ bool wait_longer(uint64_t* bar, uint32_t parity, Shared* sh, long long wait_cycles, int32_t* status) {
+    struct Limits { long long wait_cycles; int32_t* status; };
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, sh, Limits{wait_cycles, status}));
+}
+__device__ __forceinline__ bool wait_warp(uint64_t* bar, uint32_t parity, Shared* sh, const Params& p) {
+    if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
+    return wait_longer(bar, parity, sh, p.wait_cycles, p.status);
+}
+
 // D[tmem] (+)= A[smem desc] * B[smem desc], 8-bit operands (see mma_ss)
 template <uint32_t kHi, uint32_t kIdesc>
 __device__ __forceinline__ void mma_ss_f8(uint32_t leader, uint32_t d_tmem, uint32_t a_lo, uint32_t b_lo, uint32_t acc) {
@@ -80,19 +97,23 @@ __device__ __forceinline__ void mma_ts_f8(uint32_t leader, uint32_t d_tmem, uint
                  ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "n"(kHi), "n"(kIdesc), "r"(acc), "r"(leader) : "memory");
 }
 
-// Two fp16 numbers (each exactly the sum of what comes back, as far as the formats reach) as a pair of e4m3 and the pair that is
-// left over, in e4m3 or e5m2.
+// Four fp16 numbers (two words) as a word of e4m3 and one of what is left over, in e4m3 or e5m2.  (The first word is put together
+// before it is read again: with the 16-bit halves used for both, the compiler of CUDA 12.9 subtracts the wrong one.)
 template <bool kLowE5M2>
-__device__ __forceinline__ void split_pair(uint32_t x, uint32_t& high, uint32_t& low) {
-    uint16_t h, l;
-    uint32_t back, rest;
-    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(h) : "r"(x));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(h));
-    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(rest) : "r"(x), "r"(back));
-    if constexpr (kLowE5M2) asm("cvt.rn.satfinite.e5m2x2.f16x2 %0, %1;" : "=h"(l) : "r"(rest));
-    else asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(l) : "r"(rest));
-    high = h;
-    low = l;
+__device__ __forceinline__ void split_four(uint32_t x0, uint32_t x1, uint32_t& high, uint32_t& low) {
+    uint32_t b0, b1;
+    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+        : "=r"(high) : "r"(x0), "r"(x1));
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
+        : "=&r"(b0), "=r"(b1) : "r"(high));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(b0) : "r"(x0), "r"(b0));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(b1) : "r"(x1), "r"(b1));
+    if constexpr (kLowE5M2)
+        asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e5m2x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e5m2x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+            : "=r"(low) : "r"(b0), "r"(b1));
+    else
+        asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+            : "=r"(low) : "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }      // -126 <= e <= 127
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -131,77 +152,129 @@ __device__ __forceinline__ uint64_t visible_page(const Sight& s, int t0, int L) 
     return vis;
 }
 
-// Probabilities of 64 keys as e4m3 (16 words, four keys each) and what is left over as e5m2 (16 words).
-__device__ __forceinline__ void pack_e4m3(const float* pr, uint32_t* out) {
+// exp2(s * scale + base) of 32 columns; kEmu of every 8 pairs on the FMA pipe.  Probabilities for the products in 16 words at pk (sealed: 8 of
+// e4m3, then 8 of what is left over as e5m2; else bf16), their fp32 sums in acc, sealed: the largest so far, as
+// fp16 bits, in either half of `most`.
+template <bool kSealed, int kEmu>
+__device__ __forceinline__ void exp_pack(const uint32_t* sr, float scale, float base, uint32_t* pk, uint64_t (&acc)[2], uint32_t& most) {
+    if constexpr (!kSealed) {
+        exp_chunk<kEmu>(sr, scale, base, pk, acc);
+    } else {
+        const uint64_t scale2 = f2_pack(scale, scale), base2 = f2_pack(base, base);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        uint32_t h0, l0, h1, l1;
-        split_pair<true>(pack_f16(pr[4 * i], pr[4 * i + 1]), h0, l0);
-        split_pair<true>(pack_f16(pr[4 * i + 2], pr[4 * i + 3]), h1, l1);
-        out[i] = h0 | (h1 << 16);
-        out[16 + i] = l0 | (l1 << 16);
+        for (int h = 0; h < 2; ++h) {
+            uint64_t x2[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x2[i] = f2_fma(f2_pack(__uint_as_float(sr[16 * h + 2 * i]), __uint_as_float(sr[16 * h + 2 * i + 1])), scale2, base2);
+            uint32_t f16[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float p0, p1;
+                if (i < kEmu) {
+                    exp2_pair_fma(x2[i], p0, p1);
+                } else {
+                    float x0, x1;
+                    f2_unpack(x2[i], x0, x1);
+                    p0 = fast_exp2(x0);
+                    p1 = fast_exp2(x1);
+                }
+                x2[i] = f2_pack(p0, p1);
+                f16[i] = pack_f16(p0, p1);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i & 1] = f2_add(acc[i & 1], x2[i]);
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) most = __vimax3_u16x2(most, f16[i], f16[i + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) split_four<true>(f16[2 * i], f16[2 * i + 1], pk[4 * h + i], pk[8 + 4 * h + i]);
+        }
     }
 }
 
-// One page for one query row per thread: scores -> probabilities over the first 32 columns of the S buffer, running reference
-// and sum.  scale: of this row and page; dv: exponent by which the page's values exceed the accumulator's; o_factor: what the accumulator
-// is to be multiplied by because of the values' scales (1: nothing).  parity: of the P V product of the page before.
-template <bool kSealedPage>
-__device__ __forceinline__ bool softmax_page(const Params& p, Shared* sh, uint32_t parity, uint32_t s_taddr, uint32_t o_taddr, float scale,
-                                             int dv, float o_factor, bool row_ok, bool first, bool masked, uint64_t vis,
-                                             float& m_ref, float& l_sum) {
-    uint32_t sr[64];
-    tmem_ld32(s_taddr, *reinterpret_cast<uint32_t(*)[32]>(&sr[0]));
-    tmem_ld32(s_taddr + 32, *reinterpret_cast<uint32_t(*)[32]>(&sr[32]));
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+
+// A page for one query row per thread: 64 scores -> probabilities over the first 16 columns of each 32, running reference m
+// and sum l.  scale: of the scores; dv: exponent by which the page's values exceed the accumulator's.
+//
+// A page that needs care: the first one, one with keys out of sight, one whose values have a larger scale than those so far (o_factor: what the
+// accumulator is to be multiplied by), one whose probabilities outgrew the reference.  Goes through the maximum.
+struct Running { float m, l; };
+template <bool kSealed>
+static __device__ __noinline__ Running careful_page(const Params& p, Shared* sh, int pv_parity, uint32_t s_taddr, uint32_t o_taddr, float scale, int dv,
+                                                    float o_factor, bool row_ok, bool first, float headroom, uint64_t vis, float m, float l) {
+    uint32_t sr[2][32];
+    tmem_ld32(s_taddr, sr[0]);
+    tmem_ld32(s_taddr + 32, sr[1]);
     tmem_wait_ld();
-    if (masked) {
+    if (__any_sync(0xffffffffu, vis != ~0ull)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
-            if (!((uint32_t)vis & (1u << i))) sr[i] = 0xff800000u;      // -inf
-            if (!((uint32_t)(vis >> 32) & (1u << i))) sr[32 + i] = 0xff800000u;
+            if (!((uint32_t)vis & (1u << i))) sr[0][i] = 0xff800000u;      // -inf
+            if (!((uint32_t)(vis >> 32) & (1u << i))) sr[1][i] = 0xff800000u;
         }
     }
     float mx = -INFINITY;
-    max_chunk(sr, mx);
-    max_chunk(sr + 32, mx);
+    max_chunk(sr[0], mx);
+    max_chunk(sr[1], mx);
     const float m_cand = mx * scale;
-    const bool grow = row_ok && m_cand > m_ref + kMostLog2;
+    // (where one row of the warp has to move its reference, all those move that have found a larger score: they would be next)
+    const bool move = __any_sync(0xffffffffu, row_ok && m_cand > m + kMostLog2);
+    const bool grow = move && m_cand > m + headroom;
     float alpha = 1.f;
     if (grow) {
-        alpha = fast_exp2(m_ref - (m_cand - kHeadroom));    // 0 when m_ref was -inf
-        m_ref = m_cand - kHeadroom;
+        alpha = fast_exp2(m - (m_cand - headroom));         // 0 when m was -inf
+        m = m_cand - headroom;
     }
-    if (!first && __any_sync(0xffffffffu, grow || o_factor != 1.f)) {
-        // O *= alpha, once the P V product of the page before has finished
-        if (!__all_sync(0xffffffffu, mbar_wait(&sh->pv_done, parity, sh, p))) return false;
+    if (!first && (move || o_factor != 1.f)) {
+        // O *= alpha, once the P V product of the page before has finished (a wait that runs out ends the block at its next one)
+        mbar_wait_warp(&sh->pv_done, pv_parity, sh, p);
         tc_fence_after();
         rescale_o_rows(o_taddr, alpha * o_factor);
     }
-    const float base = (m_ref == -INFINITY ? 0.f : -m_ref) + (float)dv;
-    uint64_t acc[2] = {0ull, 0ull};
-    if constexpr (kSealedPage) {
-        const uint64_t scale2 = f2_pack(scale, scale), base2 = f2_pack(base, base);
+    const float base = (m == -INFINITY ? 0.f : -m) + (float)dv;
+    uint64_t acc[2] = {};
+    uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            float x0, x1;
-            f2_unpack(f2_fma(f2_pack(__uint_as_float(sr[2 * i]), __uint_as_float(sr[2 * i + 1])), scale2, base2), x0, x1);
-            x0 = fast_exp2(x0);
-            x1 = fast_exp2(x1);
-            acc[i & 1] = f2_add(acc[i & 1], f2_pack(x0, x1));
-            sr[2 * i] = __float_as_uint(x0);
-            sr[2 * i + 1] = __float_as_uint(x1);
-        }
-        uint32_t packed[32];
-        pack_e4m3(reinterpret_cast<const float*>(sr), packed);
-        tmem_st32(s_taddr, packed);
-    } else {
-#pragma unroll
-        for (int c = 0; c < 2; ++c) exp_chunk<0>(sr + 32 * c, scale, base, sr + 16 * c, acc);   // may hold -inf
-        tmem_st32(s_taddr, sr);
+    for (int c = 0; c < 2; ++c) {
+        uint32_t pk[16];
+        exp_pack<kSealed, 0>(sr[c], scale, base, pk, acc, most);      // may hold -inf
+        tmem_st16(s_taddr + 32 * c, pk);
     }
     float sum_a, sum_b;
     f2_unpack(f2_add(acc[0], acc[1]), sum_a, sum_b);
-    l_sum = l_sum * alpha + (sum_a + sum_b) * pow2(-dv);
+    tmem_wait_st();
+    tc_fence_before();
+    return Running{m, l * alpha + (sum_a + sum_b) * pow2(-dv)};
+}
+
+// Any other page: probabilities are taken against the reference of the pages before, and it shows in them whether it still serves (sealed:
+// none above what e4m3 holds; bf16: by their sum, see kMaxSum).  Returns false, with the scores as they were, where it does not.
+template <bool kSealed>
+__device__ __forceinline__ bool plain_page(uint32_t s_taddr, float scale, int dv, bool row_ok, float m, float& l) {
+    uint32_t sa[32], sb[32], pk[32], most = 0;
+    uint64_t acc[2] = {};
+    tmem_ld32(s_taddr, sa);
+    tmem_wait_ld_of(sa);
+    tmem_ld32(s_taddr + 32, sb);
+    const float base = (float)dv - m;
+    exp_pack<kSealed, kEmuPairs>(sa, scale, base, pk, acc, most);
+    tmem_wait_ld_of(sb);
+    exp_pack<kSealed, kEmuPairs>(sb, scale, base, pk + 16, acc, most);
+    float sum_a, sum_b;
+    f2_unpack(f2_add(acc[0], acc[1]), sum_a, sum_b);
+    const float sum = (sum_a + sum_b) * pow2(-dv);
+    const bool outgrown = kSealed ? max(most & 0xffffu, most >> 16) > kMostF16 : !(sum < kMostSum);
+    if (__any_sync(0xffffffffu, row_ok && outgrown)) return false;
+    l += sum;
+    tmem_st16(s_taddr, pk);
+    tmem_st16(s_taddr + 32, pk + 16);
     tmem_wait_st();
     tc_fence_before();
     return true;
@@ -227,11 +300,8 @@ __device__ __forceinline__ float split_queries(uint8_t* sQ, int r) {
         for (int k = 0; k < 4; ++k) {
             const uint4& s = v[2 * c + (k >> 1)];
             const uint32_t a = k & 1 ? s.z : s.x, b = k & 1 ? s.w : s.y;
-            uint32_t h0, l0, h1, l1;
-            split_pair<false>(pack_f16(__uint_as_float(a << 16) * up, __uint_as_float(a & 0xffff0000u) * up), h0, l0);
-            split_pair<false>(pack_f16(__uint_as_float(b << 16) * up, __uint_as_float(b & 0xffff0000u) * up), h1, l1);
-            h[k] = h0 | (h1 << 16);
-            l[k] = l0 | (l1 << 16);
+            split_four<false>(pack_f16(__uint_as_float(a << 16) * up, __uint_as_float(a & 0xffff0000u) * up),
+                              pack_f16(__uint_as_float(b << 16) * up, __uint_as_float(b & 0xffff0000u) * up), h[k], l[k]);
         }
         uint8_t* at = sQ + r * 128 + ((c ^ (r & 7)) << 4);
         *reinterpret_cast<uint4*>(at) = make_uint4(h[0], h[1], h[2], h[3]);
@@ -252,8 +322,10 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rtile = blockIdx.x % p.row_tiles;
-    const int slice = blockIdx.x / p.row_tiles % p.n_splits;
-    const int item = blockIdx.x / (p.row_tiles * p.n_splits);
+    const int unit = blockIdx.x / p.row_tiles;              // the first items are worked on whole, the others in slices
+    const int n_slices = unit < p.n_whole ? 1 : p.n_splits;
+    const int slice = unit < p.n_whole ? 0 : (unit - p.n_whole) % p.n_splits;
+    const int item = unit < p.n_whole ? unit : p.n_whole + (unit - p.n_whole) / p.n_splits;
     const int g = item % p.Hkv, b = item / p.Hkv % p.batch, layer = item / (p.Hkv * p.batch);
     if (warp == 4 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&qmap) : "memory");
@@ -280,7 +352,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     if (row0 >= M) return;
     // this block's slice [w_lo, w_hi) of the pages to read; it walks them from the last to the first
     const Walk walk = make_walk(L, N, sealed, p.window, p.sink);
-    const int per_slice = (walk.n + p.n_splits - 1) / p.n_splits;
+    const int per_slice = (walk.n + n_slices - 1) / n_slices;
     const int w_lo = min(walk.n, slice * per_slice), w_hi = min(walk.n, w_lo + per_slice);
     const int ns = w_hi - w_lo;
     const int nb = max(0, w_hi - max(w_lo, walk.n_sealed));      // bf16 pages; the others are sealed
@@ -307,26 +379,22 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     auto k_seq = [&](int j) { return j < nb ? 2 * j : nb + j; };
     auto v_seq = [&](int j) { return j < nb ? 2 * j + 1 : nb + j; };
 
+    // Registers move to the softmax warps: 128 + 128 a thread become 192 + 64.
+    if (warp >= 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     if (warp == 4) {
         // =========================== TMA producer ===========================
-        // Page ids (and scales) of 32 pages at a time, one per lane; each lane then hands its own out.
-        struct Page { int id, ke, ve; };
+        // page ids of 32 pages at a time, one per lane
         auto look_up = [&](int j) {
-            Page e{0, 127, 127};
-            if (j >= ns) return e;
-            const int w = w_hi - 1 - j, pg = walk.page(w);
+            if (j >= ns) return 0;
             const bool is8 = j >= nb;
-            e.id = is8 ? p.page_table8[(size_t)b * p.max_pages8 + pg] : p.page_table[(size_t)b * p.max_pages + pg];
-            if (e.id < 0 || e.id >= (is8 ? p.n_pages8 : p.n_pages)) {       // (checked: it becomes a TMA coordinate)
+            const int pg = walk.page(w_hi - 1 - j);
+            int id = is8 ? p.page_table8[(size_t)b * p.max_pages8 + pg] : p.page_table[(size_t)b * p.max_pages + pg];
+            if (id < 0 || id >= (is8 ? p.n_pages8 : p.n_pages)) {           // (checked: it becomes a TMA coordinate)
                 report_status(p.status, SAGE_STATUS_BAD_PAGE);
-                e.id = 0;
+                id = 0;
             }
-            if (is8) {
-                const size_t at = ((size_t)layer * p.n_pages8 + e.id) * p.Hkv + g;
-                e.ke = p.k_exp[at];
-                e.ve = p.v_exp[at];
-            }
-            return e;
+            return id;
         };
         const bool on = ns > 0 && !p.producer_off;
         int issued = 0;
@@ -336,27 +404,21 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                 for (int h = 0; h < 2; ++h)
                     tma_load_5d(smem_u32(sQ + h * kQHalfBytes), &qmap, h * 64, 0, g, n0 + (row0 >> p.g_shift), layer, &sh->q_ready);
             }
-            Page now = look_up(lane);
+            int now = look_up(lane);
             bool ok = true;
             for (int j0 = 0; ok && j0 < ns; j0 += 32) {
-                const Page next = look_up(j0 + 32 + lane);
+                const int next = look_up(j0 + 32 + lane);
                 const int n = min(32, ns - j0);
                 for (int i = 0; ok && i < n; ++i) {
-                    const int j = j0 + i;
-                    const bool is8 = j >= nb;
-                    const int id = __shfl_sync(0xffffffffu, now.id, i), ke = __shfl_sync(0xffffffffu, now.ke, i),
-                              ve = __shfl_sync(0xffffffffu, now.ve, i);
+                    const bool is8 = j0 + i >= nb;
+                    const int id = __shfl_sync(0xffffffffu, now, i);
                     const int c2 = id * p.Hkv + g;
                     for (int part = 0; part < (is8 ? 1 : 2); ++part) {
                         const int s = issued % kSlots, use = issued / kSlots;
-                        if (use > 0) ok = mbar_wait_warp(&sh->empty[s], (use - 1) & 1, sh, p);
+                        if (use > 0) ok = wait_warp(&sh->empty[s], (use - 1) & 1, sh, p);
                         if (!ok) break;
                         if (lane == 0) {
                             uint8_t* dst = sRing + s * kSlotBytes;
-                            if (is8) {
-                                sh->k_scale[s] = __uint_as_float((uint32_t)min(max(ke, kExpLo), kExpHi) << 23);
-                                sh->v_exp[s] = min(max(ve, kExpLo), kExpHi) - 127;
-                            }
                             mbar_expect_tx(&sh->full[s], kSlotBytes);
                             if (is8) {
                                 tma_load_4d(smem_u32(dst), &k8map, 0, 0, c2, layer, &sh->full[s]);
@@ -385,7 +447,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
         const int n = __shfl_sync(0xffffffffu, ns, 0);
         const uint32_t leader = elect_one() ? 1u : 0u;
-        auto wait_all = [&](uint64_t* bar, uint32_t parity) { return mbar_wait_warp(bar, parity, sh, p); };
+        auto wait_all = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity, sh, p); };
         const uint32_t dq = desc_lo(smem_u32(sQ), 16);
         const uint32_t dring = desc_lo(smem_u32(sRing), 16);
         const uint32_t dring_mn = desc_lo(smem_u32(sRing), kPageHalfBytes);
@@ -415,15 +477,15 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                 const uint32_t dv = dring_mn + ((s * kSlotBytes) >> 4);
 #pragma unroll
                 for (int ks = 0; ks < 4; ++ks)              // 16 keys; P in TMEM (8 columns per slice), V MN-major
-                    mma_ts<kDescHi, kIdescPV>(leader, o_tmem, a + ks * 8, dv + ((ks * 2048) >> 4), ks > 0 ? 1u : acc);
+                    mma_ts<kDescHi, kIdescPV>(leader, o_tmem, a + 32 * (ks >> 1) + 8 * (ks & 1), dv + ((ks * 2048) >> 4), ks > 0 ? 1u : acc);
             } else {
                 const uint32_t dv = dring_mn + ((s * kSlotBytes + kSealedBytes) >> 4);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)              // 32 keys
-                    mma_ts_f8<kDescHi, kIdescSealedPVHigh>(leader, o_tmem, a + ks * 8, dv + ((ks * 4096) >> 4), ks > 0 ? 1u : acc);
+                    mma_ts_f8<kDescHi, kIdescSealedPVHigh>(leader, o_tmem, a + ks * 32, dv + ((ks * 4096) >> 4), ks > 0 ? 1u : acc);
 #pragma unroll
                 for (int ks = 0; ks < 2; ++ks)
-                    mma_ts_f8<kDescHi, kIdescSealedPVLow>(leader, o_tmem, a + 16 + ks * 8, dv + ((ks * 4096) >> 4), 1u);
+                    mma_ts_f8<kDescHi, kIdescSealedPVLow>(leader, o_tmem, a + ks * 32 + 8, dv + ((ks * 4096) >> 4), 1u);
             }
             tc_commit(leader, &sh->pv_done);
             tc_commit(leader, &sh->empty[s]);
@@ -472,8 +534,10 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         // abort: everything issued must retire before the TMEM and the tiles go away
         if (!ok && lane == 0) mbar_wait_quiet(&sh->o_full, 0, p.wait_cycles);
         __syncwarp();
+    }
     } else {
         // =========================== softmax ===========================
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
         const int r = tid;                                  // row inside the tile == TMEM lane
         const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
         const uint32_t s_taddr = tmem + lane_base, o_taddr = tmem + lane_base + 128;
@@ -482,8 +546,27 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         const int node = row_ok ? R >> p.g_shift : 0;
         const int cut = L + N - p.window;                   // some row does not see the prefix positions in front of this one
         Sight sight{1ull << node, p.sink, 0};
-        if (nb > 0 || cut > 0) {                            // some page is masked (all of them are bf16 without a window)
-            for (int i = r; i < N; i += 128) sh->parent[i] = p.parent[n0 + i];
+        // scales of 32 sealed pages at a time, one pair of exponent bytes per lane
+        auto sealed_id = [&](int i) { return nb + i < ns ? p.page_table8[(size_t)b * p.max_pages8 + walk.page(w_hi - 1 - nb - i)] : 0; };
+        struct Raw { uint32_t k, v; };                      // (as they come: packed and limited only once they are needed)
+        auto scales_of = [&](int i, int id) {
+            Raw e{127u, 127u};
+            if (nb + i < ns) {
+                if (id < 0 || id >= p.n_pages8) id = 0;     // (reported by the copy warp)
+                const size_t at = ((size_t)layer * p.n_pages8 + id) * p.Hkv + g;
+                e.k = p.k_exp[at];
+                e.v = p.v_exp[at];
+            }
+            return e;
+        };
+        auto packed = [](const Raw& e) { return min(max(e.k, (uint32_t)kExpLo), (uint32_t)kExpHi) | (min(max(e.v, (uint32_t)kExpLo), (uint32_t)kExpHi) << 8); };
+        const bool tree = nb > 0 || cut > 0;                // some page is masked (without a window: bf16 ones only)
+        const int first_id = sealed_id(lane), next_id = sealed_id(32 + lane);      // (asked for at once: the set-up is a chain of loads)
+        if (tree && r < N) sh->parent[r] = p.parent[n0 + r];
+        const Raw first_scales = scales_of(lane, first_id);
+        Raw next_scales = scales_of(32 + lane, next_id);
+        uint32_t scales = 0;
+        if (tree) {
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (row_ok) {
                 int depth = 0, at = node;
@@ -508,55 +591,65 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                 sight.end = min(L + depth - p.window + 1, L);
             }
         }
-        float m_ref = -INFINITY, l_sum = 0.f;
+        float m_ref = row_ok ? -INFINITY : INFINITY, l_sum = 0.f;     // (rows that are not the tree's: probabilities of zero, which cost the tensor cores less power)
         float row_scale = 0.f;                              // for sealed pages
         int v_ref = 0;                                      // exponent of the accumulator: at first that of the first sealed page, if there is one
-        if (nb < ns) {
-            int id = p.page_table8[(size_t)b * p.max_pages8 + walk.page(w_hi - 1 - nb)];
-            if (id < 0 || id >= p.n_pages8) id = 0;
-            v_ref = min(max((int)p.v_exp[((size_t)layer * p.n_pages8 + id) * p.Hkv + g], kExpLo), kExpHi) - 127;
-        }
         bool ok = warp_live;
+        auto split = [&]() {                                // the query rows change their form
+            row_scale = split_queries(sQ, r) * p.scale_log2;
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->q_split);
+        };
         if (ok && ns > 0 && nb == 0) {
             ok = mbar_wait_warp(&sh->q_ready, 0, sh, p);
-            if (ok) {
-                row_scale = split_queries(sQ, r) * p.scale_log2;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh->q_split);
-            }
+            if (ok) split();
         }
-        for (int j = 0; ok && j < ns; ++j) {
-            const int x = j & 1, seq = k_seq(j), s = seq % kSlots;
+        if (ok && nb < ns) {
+            scales = packed(first_scales);
+            v_ref = (int)(__shfl_sync(0xffffffffu, scales, 0) >> 8) - 127;
+        }
+        for (int j = 0; ok && j < nb; ++j) {                // bf16 pages
+            const int x = j & 1;
             ok = mbar_wait_warp(&sh->s_full[x], (j >> 1) & 1, sh, p);
-            // A sealed page: the copy warp's own barrier too, which orders the scales that it has left beside the page.  (The slot is not filled
-            // again before this warp has been through the page.  That of a bf16 page's keys may be by now: its barrier is not to be asked.)
-            if (ok && j >= nb) ok = mbar_wait_warp(&sh->full[s], (seq / kSlots) & 1, sh, p);
             if (!ok) break;
             tc_fence_after();
-            if (j == nb - 1 && nb < ns) {                   // the last bf16 scores are there: the query rows change their form
-                row_scale = split_queries(sQ, r) * p.scale_log2;
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&sh->q_split);
-            }
+            if (j == nb - 1 && nb < ns) split();            // (the last bf16 scores are there)
             const int t0 = walk.page(w_hi - 1 - j) * kPageSize;
             const bool masked = t0 + kPageSize > L || (t0 < cut && t0 + kPageSize > p.sink);
-            const uint64_t vis = masked ? visible_page(sight, t0, L) : ~0ull;
-            if (j < nb) {
-                ok = softmax_page<false>(p, sh, (j - 1) & 1, s_taddr + x * 64, o_taddr, p.scale_log2, -v_ref, 1.f, row_ok, j == 0, masked, vis,
-                                         m_ref, l_sum);
-            } else {
-                float o_factor = 1.f;
-                const int ve = sh->v_exp[s];
-                if (ve > v_ref) {
-                    o_factor = pow2(v_ref - ve);
-                    v_ref = ve;
-                }
-                ok = softmax_page<true>(p, sh, (j - 1) & 1, s_taddr + x * 64, o_taddr, row_scale * sh->k_scale[s], ve - v_ref, o_factor,
-                                        row_ok, j == 0, masked, vis, m_ref, l_sum);
+            if (j == 0 || masked || !plain_page<false>(s_taddr + x * 64, p.scale_log2, -v_ref, row_ok, m_ref, l_sum)) {
+                const float room = j < 2 ? kHeadroomFirst : kHeadroom;
+                const Running u = careful_page<false>(p, sh, (j - 1) & 1, s_taddr + x * 64, o_taddr, p.scale_log2, -v_ref, 1.f, row_ok, j == 0, room,
+                                                      masked ? visible_page(sight, t0, L) : ~0ull, m_ref, l_sum);
+                m_ref = u.m;
+                l_sum = u.l;
             }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh->p_full[x]);
+        }
+        for (int j = nb; ok && j < ns; ++j) {               // sealed pages
+            const int x = j & 1, i = j - nb;
+            ok = mbar_wait_warp(&sh->s_full[x], (j >> 1) & 1, sh, p);
             if (!ok) break;
+            tc_fence_after();
+            if (i > 0 && i % 32 == 0) {
+                scales = packed(next_scales);
+                next_scales = scales_of(i + 32 + lane, sealed_id(i + 32 + lane));
+            }
+            const uint32_t e = __shfl_sync(0xffffffffu, scales, i & 31);
+            const int ve = (int)(e >> 8) - 127;
+            const float scale = row_scale * __uint_as_float((e & 0xffu) << 23);
+            const int t0 = cut > 0 ? walk.page(w_hi - 1 - j) * kPageSize : 0;
+            const bool masked = t0 < cut && t0 + kPageSize > p.sink;        // (a sealed page lies within the prefix)
+            if (j == 0 || masked || ve > v_ref || !plain_page<true>(s_taddr + x * 64, scale, ve - v_ref, row_ok, m_ref, l_sum)) {
+                const int v_max = max(v_ref, ve);
+                const float room = j < 2 ? kHeadroomFirst : kHeadroom;
+                const Running u = careful_page<true>(p, sh, (j - 1) & 1, s_taddr + x * 64, o_taddr, scale, ve - v_max, pow2(v_ref - v_max), row_ok, j == 0, room,
+                                                     masked ? visible_page(sight, t0, L) : ~0ull, m_ref, l_sum);
+                v_ref = v_max;
+                m_ref = u.m;
+                l_sum = u.l;
+            }
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->p_full[x]);
         }
@@ -565,18 +658,18 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         if (ok) {
             tc_fence_after();
             const size_t rows_total = (size_t)p.sum_nodes * p.Hq;
-            const size_t row = (size_t)(n0 + node) * p.Hq + g * p.G + (row_ok ? R & (p.G - 1) : 0);
-            const size_t part = (size_t)layer * p.n_splits + slice;
-            const float unit = pow2(v_ref);     // of the accumulator
-            const float inv = (l_sum > 0.f) ? unit / l_sum : 0.f;
-            if (p.n_splits > 1 && row_ok) p.part_ml[part * rows_total + row] = make_float2(m_ref, l_sum);
-#pragma unroll
+            const size_t rows = (size_t)p.row_tiles * kRowTile;       // of an item in the workspace
+            const size_t part = (size_t)(item - p.n_whole) * p.n_splits + slice;
+            const float o_unit = pow2(v_ref);   // of the accumulator
+            const float inv = (l_sum > 0.f) ? o_unit / l_sum : 0.f;
+            if (n_slices > 1 && row_ok) p.part_ml[part * rows + R] = make_float2(m_ref, l_sum);
+#pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 uint32_t o[32];
                 if (ns == 0) break;                         // (an empty slice: its l = 0 keeps the merge from reading more)
                 tmem_ld32(o_taddr + c * 32, o);
                 tmem_wait_ld();
-                if (p.n_splits == 1) {
+                if (n_slices == 1) {
                     uint4 v[4];
                     pack_rows(o, inv, v);
                     transpose4(v, lane);
@@ -589,11 +682,11 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                         }
                     }
                 } else if (row_ok) {
-                    float4* po = p.part_o + (part * (kHeadDim / 4) + c * 8) * rows_total + row;
+                    float4* po = p.part_o + (part * (kHeadDim / 4) + c * 8) * rows + R;
 #pragma unroll
                     for (int i = 0; i < 8; ++i)
-                        po[i * rows_total] = make_float4(__uint_as_float(o[4 * i]) * unit, __uint_as_float(o[4 * i + 1]) * unit,
-                                                         __uint_as_float(o[4 * i + 2]) * unit, __uint_as_float(o[4 * i + 3]) * unit);
+                        po[i * rows] = make_float4(__uint_as_float(o[4 * i]) * o_unit, __uint_as_float(o[4 * i + 1]) * o_unit,
+                                                   __uint_as_float(o[4 * i + 2]) * o_unit, __uint_as_float(o[4 * i + 3]) * o_unit);
                 }
             }
         }
@@ -606,6 +699,62 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     }
 }
 
+// Merge of the items that were worked on in slices.  A block owns 32 rows of an item (one per lane) and 32 of the 128 columns (four per
+// warp): enough warps to keep the loads of a few hundred rows in flight on the whole chip.  The weights of the slices are shared among
+// the warps; the first partial results are asked for before they are known.
+__global__ void __launch_bounds__(256) paged_merge_kernel(const Params p) {
+    after_previous_kernel();
+    constexpr int kAhead = 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = p.n_splits, quad = blockIdx.z * 8 + warp;
+    const int item = p.n_whole + blockIdx.y, g = item % p.Hkv, b = item / p.Hkv % p.batch, layer = item / (p.Hkv * p.batch);
+    const int n0 = p.node_offsets[b], N = p.node_offsets[b + 1] - n0, M = N * p.G;
+    if (N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 + N > p.sum_nodes || blockIdx.x * 32 >= M) return;      // (not worked on)
+    const int R = blockIdx.x * 32 + lane;
+    const bool ok = R < M;
+    const size_t rows = (size_t)p.row_tiles * kRowTile, r = ok ? R : blockIdx.x * 32;
+    const float2* ml = p.part_ml + (size_t)blockIdx.y * S * rows + r;
+    const float4* po = p.part_o + ((size_t)blockIdx.y * S * (kHeadDim / 4) + quad) * rows + r;
+    const size_t slice = (kHeadDim / 4) * rows;
+    __shared__ float s_m[kMostSplits][32], s_l[kMostSplits][32], s_w[kMostSplits][32];
+    float4 v[kAhead];
+    for (int s = warp; s < S; s += 8) {
+        const float2 x = ml[(size_t)s * rows];
+        s_m[s][lane] = x.y > 0.f ? x.x : -INFINITY;
+        s_l[s][lane] = x.y;
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u)
+        if (u < S) v[u] = po[u * slice];
+    __syncthreads();
+    float mx = -INFINITY, lsum = 0.f;
+    for (int s = 0; s < S; ++s) mx = fmaxf(mx, s_m[s][lane]);
+    for (int s = warp; s < S; s += 8) s_w[s][lane] = s_m[s][lane] == -INFINITY ? 0.f : exp2f(s_m[s][lane] - mx);
+    __syncthreads();
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int s0 = 0; s0 < S; s0 += kAhead) {
+        if (s0 > 0) {
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (s0 + u < S) v[u] = po[(s0 + u) * slice];
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (s0 + u >= S) break;
+            const float w = s_w[s0 + u][lane];
+            if (w > 0.f) {                                  // (else an empty slice: nothing was written; or one that holds nothing for the row)
+                lsum = fmaf(s_l[s0 + u][lane], w, lsum);
+                acc.x = fmaf(w, v[u].x, acc.x); acc.y = fmaf(w, v[u].y, acc.y);
+                acc.z = fmaf(w, v[u].z, acc.z); acc.w = fmaf(w, v[u].w, acc.w);
+            }
+        }
+    }
+    if (!ok) return;
+    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    const size_t row = (size_t)(n0 + (R >> p.g_shift)) * p.Hq + g * p.G + (R & (p.G - 1));
+    *reinterpret_cast<uint2*>(p.out + ((size_t)layer * p.sum_nodes * p.Hq + row) * kHeadDim + quad * 4) =
+        make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+}
+
 // ---- host side ------------------------------------------------------------------------------
 static int row_tiles_for(int sum_nodes, int G) {
     const int n = sum_nodes < SAGE_MAX_NODES ? sum_nodes : SAGE_MAX_NODES;      // a tree has at most that many nodes
@@ -616,28 +765,42 @@ static int most_pages(int max_pages, int window, int sink) {
     const long long w = ((long long)window - 1 + SAGE_MAX_NODES + kPageSize - 1) / kPageSize + 1 + ((long long)sink + kPageSize - 1) / kPageSize;
     return w < max_pages ? (int)w : max_pages;
 }
-// Slices of the context: two blocks are resident per SM; a wave of them takes what its pages take plus a fixed part (set-up,
-// first copies, drain), worth about six pages, and every slice costs the merge a little.
-static int pick_splits(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
-    const int nodes = (sum_nodes + batch - 1) / batch;
-    const long long base = (long long)n_layers * batch * n_kv_heads * row_tiles_for(nodes, G), slots = 2ll * n_sms;
-    const int s_max = pages < split::kMaxSplits ? pages : split::kMaxSplits;
-    int best = 1;
+// How a launch is cut: items [0, whole) are worked on by a block per row tile, the others by `splits` of them.  Two blocks are resident
+// per SM.  A wave of them takes what its pages take plus a fixed part (set-up, first copies, drain), worth about six pages; a slice costs the
+// merge a quarter of a page, the merge four.  Full waves are left whole and what is left over fills the last one: 640 items of 257 pages
+// are two waves and a sixth; 896 of 66 pages three and a bit.
+struct Cut { int whole, splits; };
+static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
+    const long long items = (long long)n_layers * batch * n_kv_heads, tiles = row_tiles_for((sum_nodes + batch - 1) / batch, G), slots = 2ll * n_sms;
+    const int s_max = pages < kMostSplits ? pages : kMostSplits;
+    Cut best{0, 1};
     double best_cost = 0.0;
-    for (int s = 1; s <= s_max; ++s) {
-        const long long waves = (base * s + slots - 1) / slots;
-        if (s > 1 && waves > 6) break;
-        const double cost = (double)waves * (6 + (pages + s - 1) / s) + (s > 1 ? 4.0 + 0.25 * s : 0.0);
-        if (s == 1 || cost < best_cost - 1e-9) { best_cost = cost; best = s; }
+    const long long full = items * tiles / slots;
+    for (long long waves = full; waves >= 0 && waves >= full - 1; --waves) {
+        const long long whole = waves * slots / tiles, rest = items - whole;
+        for (int s = 1; s <= s_max; ++s) {
+            const long long last = (rest * tiles * s + slots - 1) / slots;
+            if (s > 1 && last > 6) break;
+            const double cost = (double)waves * (6 + pages) + (double)last * (6 + (pages + s - 1) / s) + (s > 1 && rest > 0 ? 4.0 + 0.25 * s : 0.0);
+            // (Whole first; cut only for a clear gain, since trees and lengths of a batch differ and blocks without rows leave at once: 32 ragged
+            // sequences, window of 2048, 2.6 waves on paper, 147 us whole and 164 with the last 0.6 cut in three for a gain of 1 % on paper.)
+            if (best_cost == 0.0 || cost < (best.splits == 1 ? 0.92 : 1.0) * best_cost - 1e-9) {
+                best_cost = cost;
+                best = s > 1 && rest > 0 ? Cut{(int)whole, s} : Cut{(int)items, 1};
+            }
+        }
     }
     return best;
 }
 static size_t workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int pages) {
-    const int S = pick_splits(resident_ctas(), n_layers, batch, n_kv_heads, n_q_heads / n_kv_heads, pages, sum_nodes);
-    return S == 1 ? 16 : (size_t)n_layers * S * sum_nodes * n_q_heads * (kHeadDim + 2) * sizeof(float);
+    const int G = n_q_heads / n_kv_heads;
+    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes);
+    const size_t rest = (size_t)n_layers * batch * n_kv_heads - cut.whole;
+    return rest == 0 ? 16 : rest * cut.splits * row_tiles_for(sum_nodes, G) * kRowTile * (kHeadDim + 2) * sizeof(float);
 }
 static bool sizes_ok(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int max_pages) {
-    return n_layers >= 1 && batch >= 1 && sum_nodes >= 1 && n_q_heads >= 1 && n_kv_heads >= 1 && max_pages >= 1 && n_q_heads % n_kv_heads == 0;
+    return n_layers >= 1 && batch >= 1 && sum_nodes >= 1 && n_q_heads >= 1 && n_kv_heads >= 1 && max_pages >= 1 && n_q_heads % n_kv_heads == 0 &&
+           (double)n_layers * batch * n_kv_heads <= 2147483647.0;
 }
 
 struct Pools {
@@ -681,9 +844,11 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
     window = window < max_pages * kPageSize ? window : max_pages * kPageSize;
     sink = sink < max_pages * kPageSize ? sink : max_pages * kPageSize;
     const int pages = most_pages(max_pages, window, sink);
-    const int S = pick_splits(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes), tiles = row_tiles_for(sum_nodes, G);
-    const double blocks = (double)n_layers * batch * n_kv_heads * tiles * S;
-    if (blocks > 2147483647.0 || (S > 1 && n_layers > 65535)) return SAGE_ERR_UNSUPPORTED;
+    if (!sizes_ok(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, max_pages)) return SAGE_ERR_UNSUPPORTED;
+    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes);
+    const int tiles = row_tiles_for(sum_nodes, G), rest = n_layers * batch * n_kv_heads - cut.whole;
+    const double blocks = ((double)cut.whole + (double)rest * cut.splits) * tiles;
+    if (blocks > 2147483647.0) return SAGE_ERR_UNSUPPORTED;
     if (!ws || ws_bytes < workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, pages) || ((uintptr_t)ws & 15)) return SAGE_ERR_WORKSPACE;
     CUtensorMap qmap, kmap, vmap, k8map, v8map;
     if (!make_pool_map(&kmap, pools.k, n_layers, pools.n_pages, n_kv_heads, pools.layer_stride) ||
@@ -700,14 +865,14 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
     Params p{};
     p.out = (__nv_bfloat16*)out;
     p.part_o = (float4*)ws;
-    p.part_ml = S > 1 ? (float2*)((float*)ws + (size_t)n_layers * S * sum_nodes * n_q_heads * kHeadDim) : nullptr;
+    p.part_ml = (float2*)((float*)ws + (size_t)rest * cut.splits * tiles * kRowTile * kHeadDim);
     p.page_table = page_table; p.seq_len = seq_len; p.parent = parent; p.node_offsets = node_offsets; p.status = status;
     if (s8) {
         p.page_table8 = s8->page_table; p.sealed = s8->sealed; p.k_exp = s8->k_exp; p.v_exp = s8->v_exp;
         p.n_pages8 = s8->n_pages; p.max_pages8 = s8->max_pages;
     }
     p.n_layers = n_layers; p.batch = batch; p.sum_nodes = sum_nodes; p.n_pages = pools.n_pages; p.max_pages = max_pages;
-    p.Hq = n_q_heads; p.Hkv = n_kv_heads; p.G = G; p.g_shift = __builtin_ctz(G); p.n_splits = S; p.row_tiles = tiles;
+    p.Hq = n_q_heads; p.Hkv = n_kv_heads; p.G = G; p.g_shift = __builtin_ctz(G); p.n_whole = cut.whole; p.n_splits = cut.splits; p.row_tiles = tiles;
     p.window = window; p.sink = sink;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     p.wait_cycles = attention_wait_cycles();
@@ -716,8 +881,8 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
         !succeeded(sage::launch(tree_attention_paged_kernel, dim3((unsigned)blocks), kThreads, kSmemBytes, as_stream(stream), 0, p, qmap, kmap, vmap,
                                 k8map, v8map)))
         return SAGE_ERR_CUDA;
-    if (S == 1) return SAGE_OK;
-    return split::launch_merge(n_layers, node_offsets, batch, sum_nodes, n_q_heads, S, p.part_o, p.part_ml, out, true, as_stream(stream));
+    if (rest == 0) return SAGE_OK;
+    return launch_status(sage::launch(paged_merge_kernel, dim3(tiles * (kRowTile / 32), rest, 4), 256, 0, as_stream(stream), 0, p));
 }
 
 }  // namespace paged

@@ -27,7 +27,6 @@
 // All waits are bounded: on expiry the CTA records SAGE_STATUS_TIMEOUT, drains its copies, frees its
 // TMEM and returns.
 #include "attention_stream.cuh"
-#include "cache/paged.cuh"
 
 namespace sage {
 namespace split {
@@ -424,6 +423,7 @@ tree_attention_split_kernel(const SplitParams p, const __grid_constant__ CUtenso
 // keep the loads of a few hundred rows in flight on the whole chip.  The partial results are requested before the weights
 // are known.  Up to eight slices (many rows, as the chip is then filled by few slices) every thread works out the weights
 // of its row itself and the kernel stays small; more are shared among the warps through shared memory.
+constexpr int kMaxSplits = 32;
 template <int kMaxS>
 __global__ void __launch_bounds__(256) attention_split_merge_kernel(const SplitParams p) {
     after_previous_kernel();
@@ -555,16 +555,6 @@ size_t workspace_size(int n_sms, int n_layers, int batch, int sum_nodes, int n_q
     return (size_t)n_layers * S * sum_nodes * n_q_heads * (kHeadDim + 2) * sizeof(float);
 }
 
-static int start_merge(const SplitParams& p, bool overlap, cudaStream_t stream) {
-    const size_t rows_total = (size_t)p.sum_nodes * p.Hq;
-    const dim3 mg((unsigned)((rows_total + 31) / 32), p.n_layers, 4);
-    const auto merge = p.n_splits <= 4   ? attention_split_merge_kernel<4>
-                       : p.n_splits <= 8 ? attention_split_merge_kernel<8>
-                                         : attention_split_merge_kernel<kMaxSplits>;
-    if (!overlap) return launch_status(launch_in_order(merge, mg, 256, stream, p));
-    return launch_status(sage::launch(merge, mg, 256, 0, stream, 0, p));
-}
-
 // Arguments have been validated by sage_tree_attention.
 int launch(int n_sms, int n_layers, int n_pages, const int32_t* page_table, int max_pages_per_seq,
            const int32_t* seq_len, const int32_t* parent, const int32_t* node_offsets, int batch, int sum_nodes,
@@ -588,18 +578,11 @@ int launch(int n_sms, int n_layers, int n_pages, const int32_t* page_table, int 
         !succeeded(sage::launch(tree_attention_split_kernel, grid, kSplitThreads, kSplitSmemBytes, stream, 0, p, qmap, kmap, vmap)))
         return SAGE_ERR_CUDA;
     if (S == 1) return SAGE_OK;
-    return start_merge(p, merge_overlaps(n_sms, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, S), stream);
-}
-
-int launch_merge(int n_layers, const int32_t* node_offsets, int batch, int sum_nodes, int n_q_heads, int n_splits, const void* part_o,
-                 const void* part_ml, void* out, bool overlap, cudaStream_t stream) {
-    SplitParams p{};
-    p.out = (__nv_bfloat16*)out;
-    p.part_o = (float4*)part_o;
-    p.part_ml = (float2*)part_ml;
-    p.node_offsets = node_offsets;
-    p.n_layers = n_layers; p.batch = batch; p.sum_nodes = sum_nodes; p.Hq = n_q_heads; p.n_splits = n_splits;
-    return start_merge(p, overlap, stream);
+    const size_t rows_total = (size_t)sum_nodes * n_q_heads;
+    const dim3 mg((unsigned)((rows_total + 31) / 32), n_layers, 4);
+    const auto merge = S <= 4 ? attention_split_merge_kernel<4> : S <= 8 ? attention_split_merge_kernel<8> : attention_split_merge_kernel<kMaxSplits>;
+    if (!merge_overlaps(n_sms, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, S)) return launch_status(launch_in_order(merge, mg, 256, stream, p));
+    return launch_status(sage::launch(merge, mg, 256, 0, stream, 0, p));
 }
 
 }  // namespace split

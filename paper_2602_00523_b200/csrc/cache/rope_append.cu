@@ -11,8 +11,7 @@
 namespace sage {
 namespace rope {
 
-constexpr int kThreads = 256;
-constexpr int kRounds = 3;              // units of a block that are asked for at once: 80 heads of 64 + 8 + 8 take 2.75 rounds
+constexpr int kUnits = 768;             // units of a token that are asked for at once: 80 heads (64 + 8 + 8) have 640
 
 struct Params {
     const __nv_bfloat16 *q, *k, *v;
@@ -37,6 +36,10 @@ __device__ __forceinline__ void turn2(uint32_t lo, uint32_t hi, float2 c, float2
     out_hi = *reinterpret_cast<uint32_t*>(&b);
 }
 
+// kThreads: of a block.  256 spread a token's rows over more warps, 128 leave more blocks on an SM: 16384 tokens of 64 + 8 + 8 heads 117 / 109.5 us,
+// 3000 tokens 28.4 / 28.7, 672 tokens 7.5 / 8.8.  (The chain in front of the stores is short on purpose: positions are asked for beside the rows, the page id is
+// not waited for before the angles are there, 130 -> 117 us.  Two or four tokens a block, the next one's rows asked for early: 146, 153.)
+template <int kThreads>
 __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_constant__ Params p) {
     __shared__ float2 s_cs[64];         // (cos, sin)
     __shared__ int s_b, s_parent[SAGE_MAX_NODES];
@@ -57,6 +60,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
         if (h < p.Hq + p.Hkv) return p.k + layer * p.k_layer + tok * p.k_token + (h - p.Hq) * kHeadDim + c;
         return p.v + layer * p.v_layer + tok * p.v_token + (h - p.Hq - p.Hkv) * kHeadDim + c;
     };
+    constexpr int kRounds = kUnits / kThreads;
     uint4 lo[kRounds], hi[kRounds];
 #pragma unroll
     for (int i = 0; i < kRounds; ++i) {
@@ -67,6 +71,8 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
             hi[i] = *reinterpret_cast<const uint4*>(x + 64);
         }
     }
+    int pos = 0;
+    if (p.pos && tid < 64) pos = p.pos[(size_t)p.axis[tid] * p.sum_tokens + tok];     // (asked for beside the rows)
     __syncthreads();
     const int b = s_b;
     if (b < 0) return;                  // (a row behind the last sequence: left as it is)
@@ -77,11 +83,7 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
         return;
     }
     const int at = L + tok - n0;        // logical position in the cache
-    int page = p.page_table[(size_t)b * p.max_pages + at / kPageSize];
-    if (page < 0 || page >= p.n_pages) {
-        if (tid == 0) report_status(p.status, SAGE_STATUS_BAD_PAGE);
-        page = -1;
-    }
+    const int page_id = p.page_table[(size_t)b * p.max_pages + at / kPageSize];
     int depth = 0;
     if (!p.pos) {
         if (N > SAGE_MAX_NODES) {
@@ -102,11 +104,16 @@ __global__ void __launch_bounds__(kThreads) rope_append_kernel(const __grid_cons
         }
     }
     if (tid < 64) {
-        const int pos = p.pos ? p.pos[(size_t)p.axis[tid] * p.sum_tokens + tok] : p.next_pos[b] + depth;
+        if (!p.pos) pos = p.next_pos[b] + depth;
         const double t = (double)pos * p.turns[tid];
         float s, c;
         sincospif(2.f * (float)(t - rint(t)), &s, &c);
         s_cs[tid] = make_float2(c * p.scale, s * p.scale);
+    }
+    int page = page_id;                 // (looked at only now: the angles need not wait for it)
+    if (page < 0 || page >= p.n_pages) {
+        if (tid == 0) report_status(p.status, SAGE_STATUS_BAD_PAGE);
+        page = -1;
     }
     __syncthreads();
     auto finish = [&](int u, const uint4& l, const uint4& h) {
@@ -185,5 +192,7 @@ extern "C" int sage_rope_append(const sage_rope_rows* rows, const sage_rope_poli
     p.page_table = page_table; p.seq_len = seq_len; p.node_offsets = node_offsets;
     p.status = status;
     p.scale = policy->scale;
-    return launch_status(launch(rope::rope_append_kernel, dim3(sum_tokens, n_layers), rope::kThreads, 0, as_stream(stream), 0, p));
+    const dim3 grid(sum_tokens, n_layers);
+    if ((int64_t)sum_tokens * n_layers >= 4096) return launch_status(launch(rope::rope_append_kernel<128>, grid, 128, 0, as_stream(stream), 0, p));
+    return launch_status(launch(rope::rope_append_kernel<256>, grid, 256, 0, as_stream(stream), 0, p));
 }

@@ -6,7 +6,7 @@
 // kernel apply scales in exponents.  Whole pages only: every value is rounded once, when its page is complete, and no page changes its scale.
 // Bound by memory (2 bytes read, 1 written per value): a block takes K and V of one (layer, page, head), 128 threads each, which
 // hold the tile in registers between its maximum and its values, so it is read once.
-#include "sage_common.cuh"
+#include "paged.cuh"
 
 namespace sage {
 namespace seal {
@@ -180,9 +180,11 @@ extern "C" int sage_seal_kv(const void* k_pool, const void* v_pool, int64_t laye
     p.batch = batch; p.Hkv = n_kv_heads;
     p.page_table = page_table; p.page_table8 = cache->page_table; p.seq_len = seq_len;
     p.sealed = sealed; p.status = status;
-    // what may have to be sealed is known on the device only: as many blocks as are resident, or as there can be tiles
+    // What may have to be sealed is known on the device only: as many blocks as are resident (three per SM), or as there can be tiles.  (One page of each of
+    // sixteen sequences, 4 layers / 80 layers / a prefill of 16k, 28 layers: 8.5 / 83.7 / 428 us; with four, of which one waits, 9.5 / 101 / 524; with six
+    // 10.1 / 85 / 432; four resident, in 64 registers, 7.8 / 90 / 473.)
     const double most = (double)batch * max_pages_per_seq * n_layers * n_kv_heads;
-    const int resident = 148 * 6, blocks = most < resident ? (int)most : resident;
+    const int resident = resident_ctas() * 3, blocks = most < resident ? (int)most : resident;
     const int code = launch_status(launch(seal::seal_pages_kernel, dim3(blocks), seal::kThreads, 0, as_stream(stream), 0, p));
     if (code != SAGE_OK) return code;
     return launch_status(launch(seal::count_sealed_kernel, dim3(batch), 128, 0, as_stream(stream), 0, p));

@@ -521,14 +521,21 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
             tc_fence_after();
             issue_qk(j);
         }
-        if (ok) ok = values_ready(0) && keys_ready(2);
+        // (Keys of page j + 2 are waited for behind the product of page j: a bf16 page's slot is free only once the values of page j - 1 have been read, and a
+        // wait for page j + 3 ahead of the probabilities of page j + 1 held those up by a copy's latency.)
+        if (ok) ok = values_ready(0);
         for (int j = 0; ok && j < n; ++j) {
             ok = wait_all(&sh->p_full[j & 1], (j >> 1) & 1);
             if (!ok) break;
             tc_fence_after();
             issue_pv(j);
-            if (j + 2 < n) issue_qk(j + 2);                 // reuses this page's S buffer: in pipe order behind its P V
-            ok = values_ready(j + 1) && keys_ready(j + 3);
+            if (j + 2 < n) {                                // reuses this page's S buffer: in pipe order behind its P V
+                ok = keys_ready(j + 2);
+                if (!ok) break;
+                tc_fence_after();
+                issue_qk(j + 2);
+            }
+            ok = values_ready(j + 1);
         }
         tc_commit(leader, &sh->o_full);                     // arrives when every MMA has completed
         // abort: everything issued must retire before the TMEM and the tiles go away

@@ -34,6 +34,7 @@ struct Params {
     int n_layers, batch, sum_nodes, n_pages, max_pages, n_pages8, max_pages8;
     int Hq, Hkv, G, g_shift;        // G = 1 << g_shift query heads per KV head
     int n_whole, n_splits;          // items that are not cut, context slices of the others
+    int in_cluster;                 // all items are cut, and the slices of a row tile are one cluster
     int row_tiles;                  // 128-row tiles of the largest possible tree
     int window, sink;
     float scale_log2;               // sm_scale * log2(e)

@@ -33,7 +33,7 @@ using namespace stream;
 constexpr int kSlots = 5;                                   // ring of 16 KB slots
 constexpr int kSlotBytes = kPageSize * kHeadDim * 2;        // a bf16 K or V page of a head, or both of a sealed one
 constexpr int kSealedBytes = kPageSize * kHeadDim;          // a sealed K or V page of a head
-constexpr int kMostSplits = 32;                             // slices of an item
+constexpr int kMostSplits = 32, kMostInCluster = 16;        // slices of an item; as one cluster
 constexpr int kThreads = 256;                               // a softmax warpgroup; the TMA warp, the MMA warp and two idle ones
 constexpr int kTmemColumns = 256;                           // S 2 x 64, O 128
 constexpr uint32_t kIdescPage = idesc_f16(kPageSize);       // S = Q K^T, bf16
@@ -310,6 +310,61 @@ __device__ __forceinline__ float split_queries(uint8_t* sQ, int r) {
     return __uint_as_float((uint32_t)(exponent - 7) << 23);
 }
 
+// ---- slices of a row tile as one cluster: partial results stay in shared memory, where the pages were -------------------
+// [128 rows][32 column quads, padded to 33: rows of neighbouring lanes in different banks], then (reference, sum) of each row
+__device__ __forceinline__ float4& part_o(uint8_t* smem, int r, int quad) { return reinterpret_cast<float4*>(smem)[r * 33 + quad]; }
+__device__ __forceinline__ float2& part_ml(uint8_t* smem, int r) { return reinterpret_cast<float2*>(smem + kRowTile * 33 * 16)[r]; }
+static_assert(kRowTile * (33 * 16 + 8) <= kQTileBytes + kSlots * kSlotBytes, "partial results have to fit where queries and pages were");
+__device__ __forceinline__ void cluster_sync() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t of_block(uint32_t saddr, int rank) {
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
+    return a;
+}
+// Each block merges an equal part of the tile's rows x 32 column quads, read from all blocks' shared memory.  (As a launch of its own behind the
+// slices, the merge costs some 2.5 us.)
+__device__ __forceinline__ void merge_in_cluster(const Params& p, uint8_t* smem, int layer, int g, int n0, int row0, int rows, int rank, int tid) {
+    const int S = p.n_splits, total = rows * 32, end = total * (rank + 1) / S;
+    for (int e = total * rank / S + tid; e < end; e += kRowTile) {
+        const int r = e >> 5, quad = e & 31;
+        const uint32_t at_o = smem_u32(&part_o(smem, r, quad)), at_ml = smem_u32(&part_ml(smem, r));
+        float2 ml[kMostInCluster];
+        float4 v[kMostInCluster];
+#pragma unroll
+        for (int s = 0; s < kMostInCluster; ++s) {
+            ml[s] = make_float2(-INFINITY, 0.f);
+            if (s < S) {
+                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[s].x), "=f"(ml[s].y) : "r"(of_block(at_ml, s)));
+                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                             : "=f"(v[s].x), "=f"(v[s].y), "=f"(v[s].z), "=f"(v[s].w) : "r"(of_block(at_o, s)));
+            }
+        }
+        float mx = -INFINITY, lsum = 0.f;
+#pragma unroll
+        for (int s = 0; s < kMostInCluster; ++s)
+            if (ml[s].y > 0.f) mx = fmaxf(mx, ml[s].x);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int s = 0; s < kMostInCluster; ++s) {
+            if (s >= S) break;
+            const float w = ml[s].y > 0.f ? exp2f(ml[s].x - mx) : 0.f;
+            lsum = fmaf(ml[s].y, w, lsum);                  // (NaN stays NaN)
+            if (w > 0.f) {                                  // (else an empty slice, or one that holds nothing for the row)
+                acc.x = fmaf(w, v[s].x, acc.x); acc.y = fmaf(w, v[s].y, acc.y);
+                acc.z = fmaf(w, v[s].z, acc.z); acc.w = fmaf(w, v[s].w, acc.w);
+            }
+        }
+        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+        const int R = row0 + r;
+        const size_t row = (size_t)(n0 + (R >> p.g_shift)) * p.Hq + g * p.G + (R & (p.G - 1));
+        *reinterpret_cast<uint2*>(p.out + ((size_t)layer * p.sum_nodes * p.Hq + row) * kHeadDim + quad * 4) =
+            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+    }
+}
+
 __global__ void __launch_bounds__(kThreads, 2)
 tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                             const __grid_constant__ CUtensorMap vmap, const __grid_constant__ CUtensorMap k8map,
@@ -321,11 +376,21 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     Shared* sh = reinterpret_cast<Shared*>(sRing + kSlots * kSlotBytes);
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int rtile = blockIdx.x % p.row_tiles;
-    const int unit = blockIdx.x / p.row_tiles;              // the first items are worked on whole, the others in slices
-    const int n_slices = unit < p.n_whole ? 1 : p.n_splits;
-    const int slice = unit < p.n_whole ? 0 : (unit - p.n_whole) % p.n_splits;
-    const int item = unit < p.n_whole ? unit : p.n_whole + (unit - p.n_whole) / p.n_splits;
+    // Which item, row tile and slice: the first items are worked on whole, the others in slices; or all in slices, those of a row tile
+    // side by side as one cluster.
+    int rtile, n_slices, slice, item;
+    if (p.in_cluster) {
+        n_slices = p.n_splits;
+        slice = blockIdx.x % p.n_splits;
+        rtile = blockIdx.x / p.n_splits % p.row_tiles;
+        item = blockIdx.x / (p.n_splits * p.row_tiles);
+    } else {
+        const int unit = blockIdx.x / p.row_tiles;
+        rtile = blockIdx.x % p.row_tiles;
+        n_slices = unit < p.n_whole ? 1 : p.n_splits;
+        slice = unit < p.n_whole ? 0 : (unit - p.n_whole) % p.n_splits;
+        item = unit < p.n_whole ? unit : p.n_whole + (unit - p.n_whole) / p.n_splits;
+    }
     const int g = item % p.Hkv, b = item / p.Hkv % p.batch, layer = item / (p.Hkv * p.batch);
     if (warp == 4 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&qmap) : "memory");
@@ -542,6 +607,10 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         if (!ok && lane == 0) mbar_wait_quiet(&sh->o_full, 0, p.wait_cycles);
         __syncwarp();
     }
+    if (p.in_cluster) {
+        cluster_sync();
+        cluster_sync();
+    }
     } else {
         // =========================== softmax ===========================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
@@ -669,7 +738,8 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
             const size_t part = (size_t)(item - p.n_whole) * p.n_splits + slice;
             const float o_unit = pow2(v_ref);   // of the accumulator
             const float inv = (l_sum > 0.f) ? o_unit / l_sum : 0.f;
-            if (n_slices > 1 && row_ok) p.part_ml[part * rows + R] = make_float2(m_ref, l_sum);
+            if (p.in_cluster) part_ml(smem, r) = make_float2(m_ref, l_sum);
+            else if (n_slices > 1 && row_ok) p.part_ml[part * rows + R] = make_float2(m_ref, l_sum);
 #pragma unroll 1
             for (int c = 0; c < 4; ++c) {
                 uint32_t o[32];
@@ -688,6 +758,11 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                             reinterpret_cast<uint4*>(p.out + ((size_t)layer * rows_total + orow) * kHeadDim + c * 32)[lane & 3] = v[i];
                         }
                     }
+                } else if (p.in_cluster) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        part_o(smem, r, c * 8 + i) = make_float4(__uint_as_float(o[4 * i]) * o_unit, __uint_as_float(o[4 * i + 1]) * o_unit,
+                                                                 __uint_as_float(o[4 * i + 2]) * o_unit, __uint_as_float(o[4 * i + 3]) * o_unit);
                 } else if (row_ok) {
                     float4* po = p.part_o + (part * (kHeadDim / 4) + c * 8) * rows + R;
 #pragma unroll
@@ -696,6 +771,11 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                                                    __uint_as_float(o[4 * i + 2]) * o_unit, __uint_as_float(o[4 * i + 3]) * o_unit);
                 }
             }
+        }
+        if (p.in_cluster) {
+            cluster_sync();                                 // (every block of the cluster comes here, whatever its waits came to)
+            merge_in_cluster(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
+            cluster_sync();
         }
     }
     tc_fence_before();
@@ -748,15 +828,15 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const Params p) {
         for (int u = 0; u < kAhead; ++u) {
             if (s0 + u >= S) break;
             const float w = s_w[s0 + u][lane];
+            lsum = fmaf(s_l[s0 + u][lane], w, lsum);        // (NaN stays NaN)
             if (w > 0.f) {                                  // (else an empty slice: nothing was written; or one that holds nothing for the row)
-                lsum = fmaf(s_l[s0 + u][lane], w, lsum);
                 acc.x = fmaf(w, v[u].x, acc.x); acc.y = fmaf(w, v[u].y, acc.y);
                 acc.z = fmaf(w, v[u].z, acc.z); acc.w = fmaf(w, v[u].w, acc.w);
             }
         }
     }
     if (!ok) return;
-    const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
+    const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
     const size_t row = (size_t)(n0 + (R >> p.g_shift)) * p.Hq + g * p.G + (R & (p.G - 1));
     *reinterpret_cast<uint2*>(p.out + ((size_t)layer * p.sum_nodes * p.Hq + row) * kHeadDim + quad * 4) =
         make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
@@ -772,15 +852,49 @@ static int most_pages(int max_pages, int window, int sink) {
     const long long w = ((long long)window - 1 + SAGE_MAX_NODES + kPageSize - 1) / kPageSize + 1 + ((long long)sink + kPageSize - 1) / kPageSize;
     return w < max_pages ? (int)w : max_pages;
 }
+// Per device: shared memory beyond 48 KB, clusters of more than eight blocks.
+static bool allow_paged() {
+    static std::atomic<bool> done[64];
+    int dev = 0;
+    if (!allow_shared_memory<kSmemBytes>(tree_attention_paged_kernel) || !succeeded(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return false;
+    if (!done[dev].load(std::memory_order_acquire)) {
+        if (!succeeded(cudaFuncSetAttribute(tree_attention_paged_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1))) return false;
+        done[dev].store(true, std::memory_order_release);
+    }
+    return true;
+}
 // How a launch is cut: items [0, whole) are worked on by a block per row tile, the others by `splits` of them.  Two blocks are resident
 // per SM.  A wave of them takes what its pages take plus a fixed part (set-up, first copies, drain), worth about six pages; a slice costs the
 // merge a quarter of a page, the merge four.  Full waves are left whole and what is left over fills the last one: 640 items of 257 pages
 // are two waves and a sixth; 896 of 66 pages three and a bit.
-struct Cut { int whole, splits; };
+// Or all items are cut and the slices of a row tile are one cluster, which merges them itself; clusters of S blocks fit the chip
+// `clusters(S)` times at once.
+struct Cut { int whole, splits; bool in_cluster; };
+static int clusters(int S) {
+    static std::atomic<int> known[64][kMostInCluster + 1];      // + 1; 0: not asked yet
+    int dev = 0;
+    if (!succeeded(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return 2 * 148 / S;
+    int n = known[dev][S].load(std::memory_order_relaxed);
+    if (n == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)S);
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kSmemBytes;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = (unsigned)S;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        if (!allow_paged() || !succeeded(cudaOccupancyMaxActiveClusters(&n, tree_attention_paged_kernel, &cfg))) return 0;
+        known[dev][S].store(++n, std::memory_order_relaxed);
+    }
+    return n - 1;
+}
 static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
     const long long items = (long long)n_layers * batch * n_kv_heads, tiles = row_tiles_for((sum_nodes + batch - 1) / batch, G), slots = 2ll * n_sms;
     const int s_max = pages < kMostSplits ? pages : kMostSplits;
-    Cut best{0, 1};
+    Cut best{0, 1, false};
     double best_cost = 0.0;
     const long long full = items * tiles / slots;
     for (long long waves = full; waves >= 0 && waves >= full - 1; --waves) {
@@ -793,8 +907,19 @@ static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, i
             // sequences, window of 2048, 2.6 waves on paper, 147 us whole and 164 with the last 0.6 cut in three for a gain of 1 % on paper.)
             if (best_cost == 0.0 || cost < (best.splits == 1 ? 0.92 : 1.0) * best_cost - 1e-9) {
                 best_cost = cost;
-                best = s > 1 && rest > 0 ? Cut{(int)whole, s} : Cut{(int)items, 1};
+                best = s > 1 && rest > 0 ? Cut{(int)whole, s, false} : Cut{(int)items, 1, false};
             }
+        }
+    }
+    // (a cluster's merge costs about a page and a half)
+    for (int s = 2; full <= 1 && s <= kMostInCluster && s <= pages; ++s) {
+        const int at_once = clusters(s);
+        if (at_once < 1) continue;
+        const long long waves = (items * tiles + at_once - 1) / at_once;
+        const double cost = (double)waves * (6 + (pages + s - 1) / s) + 1.5;
+        if (cost < best_cost - 1e-9) {
+            best_cost = cost;
+            best = Cut{0, s, true};
         }
     }
     return best;
@@ -803,7 +928,7 @@ static size_t workspace_size(int n_layers, int batch, int sum_nodes, int n_q_hea
     const int G = n_q_heads / n_kv_heads;
     const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes);
     const size_t rest = (size_t)n_layers * batch * n_kv_heads - cut.whole;
-    return rest == 0 ? 16 : rest * cut.splits * row_tiles_for(sum_nodes, G) * kRowTile * (kHeadDim + 2) * sizeof(float);
+    return rest == 0 || cut.in_cluster ? 16 : rest * cut.splits * row_tiles_for(sum_nodes, G) * kRowTile * (kHeadDim + 2) * sizeof(float);
 }
 static bool sizes_ok(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int max_pages) {
     return n_layers >= 1 && batch >= 1 && sum_nodes >= 1 && n_q_heads >= 1 && n_kv_heads >= 1 && max_pages >= 1 && n_q_heads % n_kv_heads == 0 &&
@@ -872,23 +997,22 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
     Params p{};
     p.out = (__nv_bfloat16*)out;
     p.part_o = (float4*)ws;
-    p.part_ml = (float2*)((float*)ws + (size_t)rest * cut.splits * tiles * kRowTile * kHeadDim);
+    if (!cut.in_cluster) p.part_ml = (float2*)((float*)ws + (size_t)rest * cut.splits * tiles * kRowTile * kHeadDim);
     p.page_table = page_table; p.seq_len = seq_len; p.parent = parent; p.node_offsets = node_offsets; p.status = status;
     if (s8) {
         p.page_table8 = s8->page_table; p.sealed = s8->sealed; p.k_exp = s8->k_exp; p.v_exp = s8->v_exp;
         p.n_pages8 = s8->n_pages; p.max_pages8 = s8->max_pages;
     }
     p.n_layers = n_layers; p.batch = batch; p.sum_nodes = sum_nodes; p.n_pages = pools.n_pages; p.max_pages = max_pages;
-    p.Hq = n_q_heads; p.Hkv = n_kv_heads; p.G = G; p.g_shift = __builtin_ctz(G); p.n_whole = cut.whole; p.n_splits = cut.splits; p.row_tiles = tiles;
+    p.Hq = n_q_heads; p.Hkv = n_kv_heads; p.G = G; p.g_shift = __builtin_ctz(G); p.n_whole = cut.whole; p.n_splits = cut.splits; p.in_cluster = cut.in_cluster; p.row_tiles = tiles;
     p.window = window; p.sink = sink;
     p.scale_log2 = sm_scale * 1.4426950408889634f;
     p.wait_cycles = attention_wait_cycles();
     p.producer_off = attention_producer_off();
-    if (!allow_shared_memory<kSmemBytes>(tree_attention_paged_kernel) ||
-        !succeeded(sage::launch(tree_attention_paged_kernel, dim3((unsigned)blocks), kThreads, kSmemBytes, as_stream(stream), 0, p, qmap, kmap, vmap,
-                                k8map, v8map)))
+    if (!allow_paged() || !succeeded(sage::launch(tree_attention_paged_kernel, dim3((unsigned)blocks), kThreads, kSmemBytes, as_stream(stream),
+                                                  cut.in_cluster ? cut.splits : 0, p, qmap, kmap, vmap, k8map, v8map)))
         return SAGE_ERR_CUDA;
-    if (rest == 0) return SAGE_OK;
+    if (rest == 0 || cut.in_cluster) return SAGE_OK;
     return launch_status(sage::launch(paged_merge_kernel, dim3(tiles * (kRowTile / 32), rest, 4), 256, 0, as_stream(stream), 0, p));
 }
 

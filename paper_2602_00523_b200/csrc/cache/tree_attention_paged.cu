@@ -319,50 +319,74 @@ __device__ __forceinline__ void cluster_sync() {
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// its two halves, each by a whole warp
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 __device__ __forceinline__ uint32_t of_block(uint32_t saddr, int rank) {
     uint32_t a;
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
     return a;
 }
-// Each block merges an equal part of the tile's rows x 32 column quads, read from all blocks' shared memory.  (As a launch of its own behind the
-// slices, the merge costs some 2.5 us.)
+// Each block merges an equal part of the tile's rows x 32 column quads, read from all blocks' shared memory, kAhead slices at a time.  A thread
+// lets the others go (they may not leave before their memory has been read) as soon as it has its last values.  (As a launch of its own behind the
+// slices, the merge costs some 2.5 us more.  Eight at a time is less code to bring in for up to eight slices, 8.1 -> 7.75 us for four pages.)
+template <int kAhead>
 __device__ __forceinline__ void merge_in_cluster(const Params& p, uint8_t* smem, int layer, int g, int n0, int row0, int rows, int rank, int tid) {
     const int S = p.n_splits, total = rows * 32, end = total * (rank + 1) / S;
-    for (int e = total * rank / S + tid; e < end; e += kRowTile) {
-        const int r = e >> 5, quad = e & 31;
+    // (the same number of turns for all lanes of a warp, which arrives as a whole)
+    int left = (end - (total * rank / S + (tid & ~31)) + kRowTile - 1) / kRowTile;
+    if (left <= 0) cluster_arrive();
+    for (int at = total * rank / S + tid; left > 0; at += kRowTile, --left) {
+        const int e = min(at, end - 1), r = e >> 5, quad = e & 31;
         const uint32_t at_o = smem_u32(&part_o(smem, r, quad)), at_ml = smem_u32(&part_ml(smem, r));
-        float2 ml[kMostInCluster];
-        float4 v[kMostInCluster];
-#pragma unroll
-        for (int s = 0; s < kMostInCluster; ++s) {
-            ml[s] = make_float2(-INFINITY, 0.f);
-            if (s < S) {
-                asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[s].x), "=f"(ml[s].y) : "r"(of_block(at_ml, s)));
-                asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                             : "=f"(v[s].x), "=f"(v[s].y), "=f"(v[s].z), "=f"(v[s].w) : "r"(of_block(at_o, s)));
-            }
-        }
-        float mx = -INFINITY, lsum = 0.f;
-#pragma unroll
-        for (int s = 0; s < kMostInCluster; ++s)
-            if (ml[s].y > 0.f) mx = fmaxf(mx, ml[s].x);
+        float m = -INFINITY, l = 0.f;
         float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int s0 = 0; s0 < S; s0 += kAhead) {
+            float2 ml[kAhead];
+            float4 v[kAhead];
 #pragma unroll
-        for (int s = 0; s < kMostInCluster; ++s) {
-            if (s >= S) break;
-            const float w = ml[s].y > 0.f ? exp2f(ml[s].x - mx) : 0.f;
-            lsum = fmaf(ml[s].y, w, lsum);                  // (NaN stays NaN)
-            if (w > 0.f) {                                  // (else an empty slice, or one that holds nothing for the row)
-                acc.x = fmaf(w, v[s].x, acc.x); acc.y = fmaf(w, v[s].y, acc.y);
-                acc.z = fmaf(w, v[s].z, acc.z); acc.w = fmaf(w, v[s].w, acc.w);
+            for (int u = 0; u < kAhead; ++u) {
+                ml[u] = make_float2(-INFINITY, 0.f);
+                if (s0 + u < S) {
+                    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(ml[u].x), "=f"(ml[u].y) : "r"(of_block(at_ml, s0 + u)));
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(v[u].x), "=f"(v[u].y), "=f"(v[u].z), "=f"(v[u].w) : "r"(of_block(at_o, s0 + u)) : "memory");
+                }
+            }
+            float top = m;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+                if (ml[u].y > 0.f) top = fmaxf(top, ml[u].x);
+            if (s0 + kAhead >= S && left == 1) cluster_arrive();
+            const float old = top == -INFINITY ? 0.f : fast_exp2(m - top);
+            m = top;
+            l *= old;
+            acc.x *= old; acc.y *= old; acc.z *= old; acc.w *= old;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const float w = ml[u].y > 0.f ? fast_exp2(ml[u].x - top) : 0.f;
+                l = fmaf(ml[u].y, w, l);                    // (NaN stays NaN)
+                if (w > 0.f) {                              // (else an empty slice, or one that holds nothing for the row)
+                    acc.x = fmaf(w, v[u].x, acc.x); acc.y = fmaf(w, v[u].y, acc.y);
+                    acc.z = fmaf(w, v[u].z, acc.z); acc.w = fmaf(w, v[u].w, acc.w);
+                }
             }
         }
-        const float inv = lsum == 0.f ? 0.f : 1.f / lsum;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
         const int R = row0 + r;
         const size_t row = (size_t)(n0 + (R >> p.g_shift)) * p.Hq + g * p.G + (R & (p.G - 1));
-        *reinterpret_cast<uint2*>(p.out + ((size_t)layer * p.sum_nodes * p.Hq + row) * kHeadDim + quad * 4) =
-            make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
+        if (at < end)
+            *reinterpret_cast<uint2*>(p.out + ((size_t)layer * p.sum_nodes * p.Hq + row) * kHeadDim + quad * 4) =
+                make_uint2(pack_bf16(acc.x * inv, acc.y * inv), pack_bf16(acc.z * inv, acc.w * inv));
     }
+    cluster_wait();
 }
 
 __global__ void __launch_bounds__(kThreads, 2)
@@ -774,8 +798,9 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         }
         if (p.in_cluster) {
             cluster_sync();                                 // (every block of the cluster comes here, whatever its waits came to)
-            merge_in_cluster(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
-            cluster_sync();
+            if (n_slices <= 8) merge_in_cluster<8>(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
+            else merge_in_cluster<kMostInCluster>(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
+            __syncwarp();
         }
     }
     tc_fence_before();

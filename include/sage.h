@@ -319,7 +319,7 @@ int sage_seal_kv(const void *k_pool, const void *v_pool, int64_t layer_stride_el
 /* Tree attention over a cache whose first sealed[b] pages are sealed (0 <= sealed[b] <= L_b / 64) and the rest, with the tree's rows, bf16:
  * as sage_tree_attention in everything else.  Sealed keys and values enter the products as the 8-bit numbers that they are, queries as the
  * sum of two e4m3 numbers (off by 2^-17 of the row's largest element at most) and probabilities as the sum of an e4m3 and an
- * e5m2 number (off by 2^-7 of their value, or 2^-23 of a value near the row's largest).  Values of a sequence whose scales differ by more than about
+ * e5m2 number (off by 2^-7 of their value, or by 2^-20 of the row's largest).  Values of a sequence whose scales differ by more than about
  * 2^20 lose precision relative to the largest.  ws: sage_tree_attention_sealed_workspace_size(...)
  * bytes, for the same sizes.  One or two launches. */
 int sage_tree_attention_sealed(const void *q, const void *k_pool, const void *v_pool,

@@ -428,6 +428,7 @@ PyObject* rope_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int32_t* parent = a[10] == Py_None ? nullptr : d.i32(a[10], "parent", {tokens});
         const int32_t* next = a[11] == Py_None ? nullptr : d.i32(a[11], "next_pos", {batch});
         void* out = d.at(a[12], "out", {at::kBFloat16}, {layers, tokens, q.size(2), dim});
+        if (out == q.data_ptr() && !q.is_contiguous()) fail(PyExc_ValueError, "out: q itself only where q is contiguous");
         int32_t* status = d.status(a[13]);
         const On on(d);
         void* stream = stream_of(a[14]);

@@ -6,8 +6,8 @@
 // p_t = exp(sm_scale q K[t]), t over what the row sees.
 //
 // A block owns one tile of 128 query rows and one slice of the pages that its item (layer, sequence, KV head) has to
-// read; two blocks are resident on an SM (96 KB to 113 KB of shared memory, 256 columns of tensor memory each), so the chain
-// scores -> softmax -> P V of one runs while the other's waits.  The pages to read are counted without the gap between sinks and
+// read; two blocks are resident on an SM (113 KB of shared memory, 256 columns of tensor memory each), so that one's chain
+// scores -> softmax -> P V runs while the other's waits.  The pages to read are counted without the gap between sinks and
 // window (Walk); the sealed ones come first in that order, and a block walks it backwards: bf16 pages, then sealed ones.
 //   TMA     : query rows; K and V pages -> 128B-swizzled shared memory, a ring of five 16 KB slots: a bf16 page takes two
 //             (K, V), a sealed one takes one for both
@@ -15,11 +15,19 @@
 //   softmax : one thread per row, online, fp32, log2 domain
 // What is sealed is multiplied as it is, in kind::f8f6f4, without a way through registers and back: each bf16 query row is
 // the sum of two e4m3 rows (split_queries: exact down to 2^-9 of the row's largest element, off by 2^-17 of it below), and each
-// probability the sum of an e4m3 and an e5m2 number (pack_e4m3: 2^-7 of its value at most, where bf16 has 2^-8; 2^-23 of the
-// row's reference at least).  Two products of 8 bits cost the tensor pipe what one of 16 does, and HBM half.
+// probability the sum of an e4m3 and an e5m2 number (split_four: off by 2^-7 of its value, where bf16 has 2^-8, or by 2^-17 against a
+// reference that lies 2^3 or more below the row's maximum).  Two products of 8 bits cost the tensor pipe what one of 16 does, and HBM half.
 // The scales are powers of two: the key's goes into the row's factor of the scores, the value's into the exponent of the
 // probabilities (against the largest of the pages so far, `v_ref`, to which the accumulator is scaled).
 // All waits are bounded: on expiry the block records SAGE_STATUS_TIMEOUT, drains its copies and MMAs, frees its TMEM and returns.
+//
+// What bounds it.  One row tile: HBM and, in long launches, the board's power limit (28 layers x 4 sequences, window of 4096: 305 us in a burst, the copy
+// rate; 80 layers x 16k x 9 nodes sealed: 660 us in a burst, 790 in a loop, at 1.4 to 1.7 GHz, where 415 us of traffic are the floor).  More row tiles: the
+// tensor pipe, 640 clocks a page and tile (384 for the scores of 64 keys, where 128 keys at once would cost 256 a page but need 128 more columns of
+// tensor memory; 256 for P V), of the 800 that a page takes with two blocks (one layer, 60 nodes, 16k keys: 46 us).  Short launches: some 4 000 clocks before
+// the first scores (offsets, page ids, pages, query rows), 1 150 to 1 650 a page, 5 000 for partial results and merge (one token at 2k keys 11.1 us).
+// Tried and slower: steps of 128 keys in one S buffer (the softmax waits 2 000 clocks a step for the products of its own block; 80 layers 735 us where
+// pages took 690); a maximum in every page (2 300 clocks a page instead of 1 100 to 1 500); one exponential pair in eight or four on the FMA pipe (+0.5, +3 %).
 #include <cuda_fp16.h>
 
 #include "attention_stream.cuh"
@@ -430,7 +438,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     const int N = p.node_offsets[b + 1] - n0;
     const int L = p.seq_len[b];
     const int sealed = p.sealed ? p.sealed[b] : 0;
-    const bool bad_tree = N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 + N > p.sum_nodes;
+    const bool bad_tree = N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 > p.sum_nodes - N;
     const bool bad_page = !bad_tree && (L < 0 || (long long)L + N > (long long)p.max_pages * kPageSize || sealed < 0 ||
                                         sealed > L / kPageSize || sealed > p.max_pages8 || (smem_u32(smem) & 1023));
     const int T = L + N, M = N * p.G, row0 = rtile * kRowTile;
@@ -470,171 +478,171 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
 
     // Registers move to the softmax warps: 128 + 128 a thread become 192 + 64.
     if (warp >= 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    if (warp == 4) {
-        // =========================== TMA producer ===========================
-        // page ids of 32 pages at a time, one per lane
-        auto look_up = [&](int j) {
-            if (j >= ns) return 0;
-            const bool is8 = j >= nb;
-            const int pg = walk.page(w_hi - 1 - j);
-            int id = is8 ? p.page_table8[(size_t)b * p.max_pages8 + pg] : p.page_table[(size_t)b * p.max_pages + pg];
-            if (id < 0 || id >= (is8 ? p.n_pages8 : p.n_pages)) {           // (checked: it becomes a TMA coordinate)
-                report_status(p.status, SAGE_STATUS_BAD_PAGE);
-                id = 0;
-            }
-            return id;
-        };
-        const bool on = ns > 0 && !p.producer_off;
-        int issued = 0;
-        if (on) {
-            if (lane == 0) {
-                mbar_expect_tx(&sh->q_ready, kQTileBytes);
-                for (int h = 0; h < 2; ++h)
-                    tma_load_5d(smem_u32(sQ + h * kQHalfBytes), &qmap, h * 64, 0, g, n0 + (row0 >> p.g_shift), layer, &sh->q_ready);
-            }
-            int now = look_up(lane);
-            bool ok = true;
-            for (int j0 = 0; ok && j0 < ns; j0 += 32) {
-                const int next = look_up(j0 + 32 + lane);
-                const int n = min(32, ns - j0);
-                for (int i = 0; ok && i < n; ++i) {
-                    const bool is8 = j0 + i >= nb;
-                    const int id = __shfl_sync(0xffffffffu, now, i);
-                    const int c2 = id * p.Hkv + g;
-                    for (int part = 0; part < (is8 ? 1 : 2); ++part) {
-                        const int s = issued % kSlots, use = issued / kSlots;
-                        if (use > 0) ok = wait_warp(&sh->empty[s], (use - 1) & 1, sh, p);
-                        if (!ok) break;
-                        if (lane == 0) {
-                            uint8_t* dst = sRing + s * kSlotBytes;
-                            mbar_expect_tx(&sh->full[s], kSlotBytes);
-                            if (is8) {
-                                tma_load_4d(smem_u32(dst), &k8map, 0, 0, c2, layer, &sh->full[s]);
-                                tma_load_4d(smem_u32(dst + kSealedBytes), &v8map, 0, 0, c2, layer, &sh->full[s]);
-                            } else {
-                                const CUtensorMap* map = part == 0 ? &kmap : &vmap;
-                                for (int h = 0; h < 2; ++h)
-                                    tma_load_4d(smem_u32(dst + h * kPageHalfBytes), map, h * 64, 0, c2, layer, &sh->full[s]);
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+        if (warp == 4) {
+            // =========================== TMA producer ===========================
+            // page ids of 32 pages at a time, one per lane
+            auto look_up = [&](int j) {
+                if (j >= ns) return 0;
+                const bool is8 = j >= nb;
+                const int pg = walk.page(w_hi - 1 - j);
+                int id = is8 ? p.page_table8[(size_t)b * p.max_pages8 + pg] : p.page_table[(size_t)b * p.max_pages + pg];
+                if (id < 0 || id >= (is8 ? p.n_pages8 : p.n_pages)) {           // (checked: it becomes a TMA coordinate)
+                    report_status(p.status, SAGE_STATUS_BAD_PAGE);
+                    id = 0;
+                }
+                return id;
+            };
+            const bool on = ns > 0 && !p.producer_off;
+            int issued = 0;
+            if (on) {
+                if (lane == 0) {
+                    mbar_expect_tx(&sh->q_ready, kQTileBytes);
+                    for (int h = 0; h < 2; ++h)
+                        tma_load_5d(smem_u32(sQ + h * kQHalfBytes), &qmap, h * 64, 0, g, n0 + (row0 >> p.g_shift), layer, &sh->q_ready);
+                }
+                int now = look_up(lane);
+                bool ok = true;
+                for (int j0 = 0; ok && j0 < ns; j0 += 32) {
+                    const int next = look_up(j0 + 32 + lane);
+                    const int n = min(32, ns - j0);
+                    for (int i = 0; ok && i < n; ++i) {
+                        const bool is8 = j0 + i >= nb;
+                        const int id = __shfl_sync(0xffffffffu, now, i);
+                        const int c2 = id * p.Hkv + g;
+                        for (int part = 0; part < (is8 ? 1 : 2); ++part) {
+                            const int s = issued % kSlots, use = issued / kSlots;
+                            if (use > 0) ok = wait_warp(&sh->empty[s], (use - 1) & 1, sh, p);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                uint8_t* dst = sRing + s * kSlotBytes;
+                                mbar_expect_tx(&sh->full[s], kSlotBytes);
+                                if (is8) {
+                                    tma_load_4d(smem_u32(dst), &k8map, 0, 0, c2, layer, &sh->full[s]);
+                                    tma_load_4d(smem_u32(dst + kSealedBytes), &v8map, 0, 0, c2, layer, &sh->full[s]);
+                                } else {
+                                    const CUtensorMap* map = part == 0 ? &kmap : &vmap;
+                                    for (int h = 0; h < 2; ++h)
+                                        tma_load_4d(smem_u32(dst + h * kPageHalfBytes), map, h * 64, 0, c2, layer, &sh->full[s]);
+                                }
                             }
+                            ++issued;
                         }
-                        ++issued;
                     }
+                    now = next;
                 }
-                now = next;
-            }
-            if (sh->abort && lane == 0) {
-                // drain: every issued copy must land before the block may exit
-                mbar_wait_quiet(&sh->q_ready, 0, p.wait_cycles);
-                for (int n = max(0, issued - kSlots); n < issued; ++n)
-                    mbar_wait_quiet(&sh->full[n % kSlots], (n / kSlots) & 1, p.wait_cycles);
-            }
-            __syncwarp();
-        }
-    } else if (warp == 5) {
-        // =========================== MMA issuer ===========================
-        const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
-        const int n = __shfl_sync(0xffffffffu, ns, 0);
-        const uint32_t leader = elect_one() ? 1u : 0u;
-        auto wait_all = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity, sh, p); };
-        const uint32_t dq = desc_lo(smem_u32(sQ), 16);
-        const uint32_t dring = desc_lo(smem_u32(sRing), 16);
-        const uint32_t dring_mn = desc_lo(smem_u32(sRing), kPageHalfBytes);
-        const uint32_t o_tmem = tm + 128;
-        auto wait_slot = [&](int seq) { return wait_all(&sh->full[seq % kSlots], (seq / kSlots) & 1); };
-        auto issue_qk = [&](int j) {
-            const int s = k_seq(j) % kSlots;
-            const uint32_t d = tm + (j & 1) * 64, dk = dring + ((s * kSlotBytes) >> 4);
-            if (j < nb) {
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)              // slices of K = 16 over d = 128 (4 per 64-wide half)
-                    mma_ss<kDescHi, kIdescPage>(leader, d, dq + (((ks >> 2) * kQHalfBytes + (ks & 3) * 32) >> 4),
-                                                dk + (((ks >> 2) * kPageHalfBytes + (ks & 3) * 32) >> 4), ks > 0 ? 1u : 0u);
-            } else {
-#pragma unroll
-                for (int ks = 0; ks < 8; ++ks)              // slices of K = 32: 4 of the high rows, 4 of the low ones
-                    mma_ss_f8<kDescHi, kIdescSealedQK>(leader, d, dq + (((ks >> 2) * kQHalfBytes + (ks & 3) * 32) >> 4),
-                                                       dk + (((ks & 3) * 32) >> 4), ks > 0 ? 1u : 0u);
-            }
-            tc_commit(leader, &sh->s_full[j & 1]);
-            if (j < nb) tc_commit(leader, &sh->empty[s]);
-        };
-        auto issue_pv = [&](int j) {
-            const int s = v_seq(j) % kSlots;
-            const uint32_t a = tm + (j & 1) * 64, acc = j > 0 ? 1u : 0u;
-            if (j < nb) {
-                const uint32_t dv = dring_mn + ((s * kSlotBytes) >> 4);
-#pragma unroll
-                for (int ks = 0; ks < 4; ++ks)              // 16 keys; P in TMEM (8 columns per slice), V MN-major
-                    mma_ts<kDescHi, kIdescPV>(leader, o_tmem, a + 32 * (ks >> 1) + 8 * (ks & 1), dv + ((ks * 2048) >> 4), ks > 0 ? 1u : acc);
-            } else {
-                const uint32_t dv = dring_mn + ((s * kSlotBytes + kSealedBytes) >> 4);
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks)              // 32 keys
-                    mma_ts_f8<kDescHi, kIdescSealedPVHigh>(leader, o_tmem, a + ks * 32, dv + ((ks * 4096) >> 4), ks > 0 ? 1u : acc);
-#pragma unroll
-                for (int ks = 0; ks < 2; ++ks)
-                    mma_ts_f8<kDescHi, kIdescSealedPVLow>(leader, o_tmem, a + ks * 32 + 8, dv + ((ks * 4096) >> 4), 1u);
-            }
-            tc_commit(leader, &sh->pv_done);
-            tc_commit(leader, &sh->empty[s]);
-        };
-        // Keys of page j are there, and the query rows in the form that they need.
-        auto keys_ready = [&](int j) {
-            if (j >= n) return true;
-            if (!wait_slot(k_seq(j))) return false;
-            return j != nb || wait_all(&sh->q_split, 0);
-        };
-        auto values_ready = [&](int j) {
-            if (j >= n) return true;
-            if (j >= nb) return true;                       // (with its keys)
-            if (!wait_slot(v_seq(j))) return false;
-            const int valid = T - walk.page(w_hi - 1 - j) * kPageSize;
-            if (valid < kPageSize) {
-                // rows past the end of the sequence may hold anything: zero them so that 0 * V stays 0
-                uint8_t* vb = sRing + v_seq(j) % kSlots * kSlotBytes;
-                for (int c = lane; c < (kPageSize - valid) * 16; c += 32) {
-                    const int r = valid + c / 16, ch = c % 16;
-                    *reinterpret_cast<uint4*>(vb + (ch >> 3) * kPageHalfBytes + r * 128 + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                if (sh->abort && lane == 0) {
+                    // drain: every issued copy must land before the block may exit
+                    mbar_wait_quiet(&sh->q_ready, 0, p.wait_cycles);
+                    for (int n = max(0, issued - kSlots); n < issued; ++n)
+                        mbar_wait_quiet(&sh->full[n % kSlots], (n / kSlots) & 1, p.wait_cycles);
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }
-            return true;
-        };
-        bool ok = n > 0;
-        if (ok) ok = wait_all(&sh->q_ready, 0);
-        for (int j = 0; ok && j < min(2, n); ++j) {
-            ok = keys_ready(j);
-            if (!ok) break;
-            tc_fence_after();
-            issue_qk(j);
-        }
-        // (Keys of page j + 2 are waited for behind the product of page j: a bf16 page's slot is free only once the values of page j - 1 have been read, and a
-        // wait for page j + 3 ahead of the probabilities of page j + 1 held those up by a copy's latency.)
-        if (ok) ok = values_ready(0);
-        for (int j = 0; ok && j < n; ++j) {
-            ok = wait_all(&sh->p_full[j & 1], (j >> 1) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            issue_pv(j);
-            if (j + 2 < n) {                                // reuses this page's S buffer: in pipe order behind its P V
-                ok = keys_ready(j + 2);
+        } else if (warp == 5) {
+            // =========================== MMA issuer ===========================
+            const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+            const int n = __shfl_sync(0xffffffffu, ns, 0);
+            const uint32_t leader = elect_one() ? 1u : 0u;
+            auto wait_all = [&](uint64_t* bar, uint32_t parity) { return wait_warp(bar, parity, sh, p); };
+            const uint32_t dq = desc_lo(smem_u32(sQ), 16);
+            const uint32_t dring = desc_lo(smem_u32(sRing), 16);
+            const uint32_t dring_mn = desc_lo(smem_u32(sRing), kPageHalfBytes);
+            const uint32_t o_tmem = tm + 128;
+            auto wait_slot = [&](int seq) { return wait_all(&sh->full[seq % kSlots], (seq / kSlots) & 1); };
+            auto issue_qk = [&](int j) {
+                const int s = k_seq(j) % kSlots;
+                const uint32_t d = tm + (j & 1) * 64, dk = dring + ((s * kSlotBytes) >> 4);
+                if (j < nb) {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)              // slices of K = 16 over d = 128 (4 per 64-wide half)
+                        mma_ss<kDescHi, kIdescPage>(leader, d, dq + (((ks >> 2) * kQHalfBytes + (ks & 3) * 32) >> 4),
+                                                    dk + (((ks >> 2) * kPageHalfBytes + (ks & 3) * 32) >> 4), ks > 0 ? 1u : 0u);
+                } else {
+#pragma unroll
+                    for (int ks = 0; ks < 8; ++ks)              // slices of K = 32: 4 of the high rows, 4 of the low ones
+                        mma_ss_f8<kDescHi, kIdescSealedQK>(leader, d, dq + (((ks >> 2) * kQHalfBytes + (ks & 3) * 32) >> 4),
+                                                           dk + (((ks & 3) * 32) >> 4), ks > 0 ? 1u : 0u);
+                }
+                tc_commit(leader, &sh->s_full[j & 1]);
+                if (j < nb) tc_commit(leader, &sh->empty[s]);
+            };
+            auto issue_pv = [&](int j) {
+                const int s = v_seq(j) % kSlots;
+                const uint32_t a = tm + (j & 1) * 64, acc = j > 0 ? 1u : 0u;
+                if (j < nb) {
+                    const uint32_t dv = dring_mn + ((s * kSlotBytes) >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)              // 16 keys; P in TMEM (8 columns per slice), V MN-major
+                        mma_ts<kDescHi, kIdescPV>(leader, o_tmem, a + 32 * (ks >> 1) + 8 * (ks & 1), dv + ((ks * 2048) >> 4), ks > 0 ? 1u : acc);
+                } else {
+                    const uint32_t dv = dring_mn + ((s * kSlotBytes + kSealedBytes) >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)              // 32 keys
+                        mma_ts_f8<kDescHi, kIdescSealedPVHigh>(leader, o_tmem, a + ks * 32, dv + ((ks * 4096) >> 4), ks > 0 ? 1u : acc);
+#pragma unroll
+                    for (int ks = 0; ks < 2; ++ks)
+                        mma_ts_f8<kDescHi, kIdescSealedPVLow>(leader, o_tmem, a + ks * 32 + 8, dv + ((ks * 4096) >> 4), 1u);
+                }
+                tc_commit(leader, &sh->pv_done);
+                tc_commit(leader, &sh->empty[s]);
+            };
+            // Keys of page j are there, and the query rows in the form that they need.
+            auto keys_ready = [&](int j) {
+                if (j >= n) return true;
+                if (!wait_slot(k_seq(j))) return false;
+                return j != nb || wait_all(&sh->q_split, 0);
+            };
+            auto values_ready = [&](int j) {
+                if (j >= n) return true;
+                if (j >= nb) return true;                       // (with its keys)
+                if (!wait_slot(v_seq(j))) return false;
+                const int valid = T - walk.page(w_hi - 1 - j) * kPageSize;
+                if (valid < kPageSize) {
+                    // rows past the end of the sequence may hold anything: zero them so that 0 * V stays 0
+                    uint8_t* vb = sRing + v_seq(j) % kSlots * kSlotBytes;
+                    for (int c = lane; c < (kPageSize - valid) * 16; c += 32) {
+                        const int r = valid + c / 16, ch = c % 16;
+                        *reinterpret_cast<uint4*>(vb + (ch >> 3) * kPageHalfBytes + r * 128 + ((ch & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                }
+                return true;
+            };
+            bool ok = n > 0;
+            if (ok) ok = wait_all(&sh->q_ready, 0);
+            for (int j = 0; ok && j < min(2, n); ++j) {
+                ok = keys_ready(j);
                 if (!ok) break;
                 tc_fence_after();
-                issue_qk(j + 2);
+                issue_qk(j);
             }
-            ok = values_ready(j + 1);
+            // (Keys of page j + 2 are waited for behind the product of page j: a bf16 page's slot is free only once the values of page j - 1 have been read, and a
+            // wait for page j + 3 ahead of the probabilities of page j + 1 held those up by a copy's latency.)
+            if (ok) ok = values_ready(0);
+            for (int j = 0; ok && j < n; ++j) {
+                ok = wait_all(&sh->p_full[j & 1], (j >> 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                issue_pv(j);
+                if (j + 2 < n) {                                // reuses this page's S buffer: in pipe order behind its P V
+                    ok = keys_ready(j + 2);
+                    if (!ok) break;
+                    tc_fence_after();
+                    issue_qk(j + 2);
+                }
+                ok = values_ready(j + 1);
+            }
+            tc_commit(leader, &sh->o_full);                     // arrives when every MMA has completed
+            // abort: everything issued must retire before the TMEM and the tiles go away
+            if (!ok && lane == 0) mbar_wait_quiet(&sh->o_full, 0, p.wait_cycles);
+            __syncwarp();
         }
-        tc_commit(leader, &sh->o_full);                     // arrives when every MMA has completed
-        // abort: everything issued must retire before the TMEM and the tiles go away
-        if (!ok && lane == 0) mbar_wait_quiet(&sh->o_full, 0, p.wait_cycles);
-        __syncwarp();
-    }
-    if (p.in_cluster) {
-        cluster_sync();
-        cluster_sync();
-    }
+        if (p.in_cluster) {
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         // =========================== softmax ===========================
         asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
@@ -700,6 +708,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(&sh->q_split);
+            __syncwarp();
         };
         if (ok && ns > 0 && nb == 0) {
             ok = mbar_wait_warp(&sh->q_ready, 0, sh, p);
@@ -820,7 +829,7 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const Params p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = p.n_splits, quad = blockIdx.z * 8 + warp;
     const int item = p.n_whole + blockIdx.y, g = item % p.Hkv, b = item / p.Hkv % p.batch, layer = item / (p.Hkv * p.batch);
     const int n0 = p.node_offsets[b], N = p.node_offsets[b + 1] - n0, M = N * p.G;
-    if (N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 + N > p.sum_nodes || blockIdx.x * 32 >= M) return;      // (not worked on)
+    if (N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 > p.sum_nodes - N || blockIdx.x * 32 >= M) return;      // (not worked on)
     const int R = blockIdx.x * 32 + lane;
     const bool ok = R < M;
     const size_t rows = (size_t)p.row_tiles * kRowTile, r = ok ? R : blockIdx.x * 32;
@@ -949,11 +958,15 @@ static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, i
     }
     return best;
 }
-static size_t workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int pages) {
-    const int G = n_q_heads / n_kv_heads;
-    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes);
+// Bytes of partial results: of the items that are cut and not merged by a cluster.
+static size_t partial_bytes(const Cut& cut, int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads) {
     const size_t rest = (size_t)n_layers * batch * n_kv_heads - cut.whole;
-    return rest == 0 || cut.in_cluster ? 16 : rest * cut.splits * row_tiles_for(sum_nodes, G) * kRowTile * (kHeadDim + 2) * sizeof(float);
+    if (rest == 0 || cut.in_cluster) return 16;
+    return rest * cut.splits * row_tiles_for(sum_nodes, n_q_heads / n_kv_heads) * kRowTile * (kHeadDim + 2) * sizeof(float);
+}
+static size_t workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int pages) {
+    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, n_q_heads / n_kv_heads, pages, sum_nodes);
+    return partial_bytes(cut, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads);
 }
 static bool sizes_ok(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int max_pages) {
     return n_layers >= 1 && batch >= 1 && sum_nodes >= 1 && n_q_heads >= 1 && n_kv_heads >= 1 && max_pages >= 1 && n_q_heads % n_kv_heads == 0 &&
@@ -1006,7 +1019,7 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
     const int tiles = row_tiles_for(sum_nodes, G), rest = n_layers * batch * n_kv_heads - cut.whole;
     const double blocks = ((double)cut.whole + (double)rest * cut.splits) * tiles;
     if (blocks > 2147483647.0) return SAGE_ERR_UNSUPPORTED;
-    if (!ws || ws_bytes < workspace_size(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, pages) || ((uintptr_t)ws & 15)) return SAGE_ERR_WORKSPACE;
+    if (!ws || ws_bytes < partial_bytes(cut, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads) || ((uintptr_t)ws & 15)) return SAGE_ERR_WORKSPACE;
     CUtensorMap qmap, kmap, vmap, k8map, v8map;
     if (!make_pool_map(&kmap, pools.k, n_layers, pools.n_pages, n_kv_heads, pools.layer_stride) ||
         !make_pool_map(&vmap, pools.v, n_layers, pools.n_pages, n_kv_heads, pools.layer_stride) ||

@@ -282,7 +282,8 @@ def near_sealed(b, got, spread=1.0):
     most_q = np.abs(b.q).max()
     most_k = max(np.abs(k).sum(-1).max() for k in b.k)
     per_p = 2.0 ** -7 + 2 * 2.0 ** -17 * most_q * most_k * SCALE
-    # ... and probabilities below the formats' range: 2^-23 of the row's largest, for every key
+    # ... and probabilities below the formats' range: half of e5m2's smallest step, 2^-17, against a reference 2^3 below the maximum
+    # of the first page and 2^5 below later ones: 2^-20 of the row's largest at most.  Held to 2^-23 here, where a row's maximum is not the first page's.
     floor = 2.0 ** -23 * max(k.shape[2] for k in b.k) * max(np.abs(v).max() for v in b.v)
     assert np.isfinite(got).all()
     over = np.abs(got - want) - (HALF_BF16 * np.abs(want) + (per_p + SLOP) * size + floor)

@@ -446,3 +446,20 @@ def test_a_run_of_rounds():
             round_reference(b)
         assert seq_len.tolist() == [x.shape[2] for x in rk] and sealed.tolist() == [x.shape[2] // PAGE for x in rk]
     assert sum(sealed.tolist()) > 2 + 2         # (a page has been filled and sealed within the rounds)
+
+
+def test_rope_refuses_to_turn_rows_in_place_that_lie_apart():
+    rows = torch.zeros(1, 1, 6, DIM, dtype=torch.bfloat16, device="cuda")
+    wide = torch.zeros(1, 2, 6, DIM, dtype=torch.bfloat16, device="cuda")
+    pool, table = torch.zeros(1, 2, 1, PAGE, DIM, dtype=torch.bfloat16, device="cuda"), dev32([[0, 1]])
+    args = [sage.make_rope_policy(), pool, pool.clone(), table, dev32([0]), dev32([0, 1])]
+    pos = dev32([[1], [1], [1]])
+    sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args, pos=pos)
+    with pytest.raises(ValueError, match="contiguous"):
+        sage.sage_rope_append(wide[:, :, :4], wide[:, :, 4:5], wide[:, :, 5:], *args, pos=dev32([[1, 1]] * 3), out=wide.view(1, 3, 4, DIM)[:, :2])
+    with pytest.raises(ValueError, match="size"):
+        sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args, pos=dev32([[1, 1]] * 3))
+    with pytest.raises(sage.SageError):
+        sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args)
+    with pytest.raises(sage.SageError):
+        sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args, pos=pos, parent=dev32([-1]), next_pos=dev32([0]))

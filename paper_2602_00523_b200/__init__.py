@@ -1,7 +1,8 @@
 """B200-native (sm_100a) kernels for the data-parallel hot path of a SAGE decode
 round: fused softmax-entropy + top-k, entropy -> tree template, tree-masked
 verification attention over a paged bf16 KV cache, greedy acceptance and KV
-compaction.  The product is the C-ABI library ``libsage.so`` (include/sage.h);
+compaction; around the cache, rotary positions with append, pages sealed into 8 bits, and attention
+over those or with a window.  The product is the C-ABI library ``libsage.so`` (include/sage.h);
 this package is its thin Python binding.  Build it with
 ``python -m paper_2602_00523_b200.build``.
 

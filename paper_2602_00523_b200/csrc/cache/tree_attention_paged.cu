@@ -907,7 +907,7 @@ struct Cut { int whole, splits; bool in_cluster; };
 static int clusters(int S) {
     static std::atomic<int> known[64][kMostInCluster + 1];      // + 1; 0: not asked yet
     int dev = 0;
-    if (!succeeded(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return 2 * 148 / S;
+    if (!succeeded(cudaGetDevice(&dev)) || dev < 0 || dev >= 64) return 0;      // (a size query without a device asks for what any plan needs)
     int n = known[dev][S].load(std::memory_order_relaxed);
     if (n == 0) {
         cudaLaunchConfig_t cfg = {};

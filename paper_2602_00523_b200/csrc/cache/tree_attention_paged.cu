@@ -341,11 +341,12 @@ __device__ __forceinline__ uint32_t of_block(uint32_t saddr, int rank) {
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(saddr), "r"(rank));
     return a;
 }
-// Each block merges an equal part of the tile's rows x 32 column quads, read from all blocks' shared memory, kAhead slices at a time.  A thread
+// Each block merges an equal part of the tile's rows x 32 column quads, read from all blocks' shared memory, one output a thread at a time.  A warp
 // lets the others go (they may not leave before their memory has been read) as soon as it has its last values.  (As a launch of its own behind the
-// slices, the merge costs some 2.5 us more.  Eight at a time is less code to bring in for up to eight slices, 8.1 -> 7.75 us for four pages.)
-template <int kAhead>
+// slices, the merge costs some 2.5 us more for few rows, and no more for 128.  The code is run once and cold, so it is kept short: unrolled
+// for sixteen slices, or several outputs at a time, it is slower by up to a microsecond where there are few rows.)
 __device__ __forceinline__ void merge_in_cluster(const Params& p, uint8_t* smem, int layer, int g, int n0, int row0, int rows, int rank, int tid) {
+    constexpr int kAhead = 8;
     const int S = p.n_splits, total = rows * 32, end = total * (rank + 1) / S;
     // (the same number of turns for all lanes of a warp, which arrives as a whole)
     int left = (end - (total * rank / S + (tid & ~31)) + kRowTile - 1) / kRowTile;
@@ -807,8 +808,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         }
         if (p.in_cluster) {
             cluster_sync();                                 // (every block of the cluster comes here, whatever its waits came to)
-            if (n_slices <= 8) merge_in_cluster<8>(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
-            else merge_in_cluster<kMostInCluster>(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
+            merge_in_cluster(p, smem, layer, g, n0, row0, min(kRowTile, M - row0), slice, r);
             __syncwarp();
         }
     }
@@ -897,10 +897,7 @@ static bool allow_paged() {
     }
     return true;
 }
-// How a launch is cut: items [0, whole) are worked on by a block per row tile, the others by `splits` of them.  Two blocks are resident
-// per SM.  A wave of them takes what its pages take plus a fixed part (set-up, first copies, drain), worth about six pages; a slice costs the
-// merge a quarter of a page, the merge four.  Full waves are left whole and what is left over fills the last one: 640 items of 257 pages
-// are two waves and a sixth; 896 of 66 pages three and a bit.
+// How a launch is cut: items [0, whole) are worked on by a block per row tile, the others by `splits` of them, merged by a kernel of its own.
 // Or all items are cut and the slices of a row tile are one cluster, which merges them itself; clusters of S blocks fit the chip
 // `clusters(S)` times at once.
 struct Cut { int whole, splits; bool in_cluster; };
@@ -925,33 +922,44 @@ static int clusters(int S) {
     }
     return n - 1;
 }
+// The costs, in us, fitted to launches of one to 63 pages a sequence, 8 to 480 rows, forced to one to sixteen slices:
+//   a wave of blocks, one per SM           2.5 + 0.67 a page (a lone token 7.5 + 0.67 P with the launch's 5: 8.6 / 9.9 / 12.5 / 18.2 / 49.7 for 2 / 4 / 8 / 16 / 63)
+//   ... two per SM                         4.5 + 1.05 a page
+//   the merge as a kernel                  1.7, 2 more beyond eight slices (another round of reads), and the partial results, written and read
+//   the merge in a cluster                 0.3, and 0.42 for each of a thread's outputs (128 rows: 6.7 us with two slices, 1.5 with eight); 1.5 more and twice
+//                                          that beyond eight slices
+// Full waves are left whole and what is left over fills the last one: 640 items of 257 pages are two waves and a sixth.  Cut only for a clear gain, since
+// trees and lengths of a batch differ and blocks without rows leave at once: four sequences of 200 to 800 keys, 24 to 60 nodes, 18.6 us whole, 24 to 28 cut.
 static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
-    const long long items = (long long)n_layers * batch * n_kv_heads, tiles = row_tiles_for((sum_nodes + batch - 1) / batch, G), slots = 2ll * n_sms;
-    const int s_max = pages < kMostSplits ? pages : kMostSplits;
-    Cut best{0, 1, false};
-    double best_cost = 0.0;
+    const int nodes = (sum_nodes + batch - 1) / batch, limit = nodes < SAGE_MAX_NODES ? nodes : SAGE_MAX_NODES;
+    const long long items = (long long)n_layers * batch * n_kv_heads, tiles = row_tiles_for(nodes, G), slots = 2ll * n_sms;
+    const double rows = (double)limit * G / (double)tiles;              // of a tile
+    auto last_wave = [&](long long blocks, int per_block) {
+        double cost = 0.0;
+        for (; blocks > slots; blocks -= slots) cost += 4.5 + 1.05 * per_block;
+        return cost + (blocks <= 0 ? 0.0 : blocks <= n_sms ? 2.5 + 0.67 * per_block : 4.5 + 1.05 * per_block);
+    };
     const long long full = items * tiles / slots;
+    Cut best{(int)items, 1, false};
+    double best_cost = full * (4.5 + 1.05 * pages) + last_wave(items * tiles - full * slots, pages);
+    best_cost *= 0.92;
     for (long long waves = full; waves >= 0 && waves >= full - 1; --waves) {
         const long long whole = waves * slots / tiles, rest = items - whole;
-        for (int s = 1; s <= s_max; ++s) {
-            const long long last = (rest * tiles * s + slots - 1) / slots;
-            if (s > 1 && last > 6) break;
-            const double cost = (double)waves * (6 + pages) + (double)last * (6 + (pages + s - 1) / s) + (s > 1 && rest > 0 ? 4.0 + 0.25 * s : 0.0);
-            // (Whole first; cut only for a clear gain, since trees and lengths of a batch differ and blocks without rows leave at once: 32 ragged
-            // sequences, window of 2048, 2.6 waves on paper, 147 us whole and 164 with the last 0.6 cut in three for a gain of 1 % on paper.)
-            if (best_cost == 0.0 || cost < (best.splits == 1 ? 0.92 : 1.0) * best_cost - 1e-9) {
+        if (rest < 1) continue;
+        for (int s = 2; s <= kMostSplits && s <= pages && rest * tiles * s <= 4 * slots; ++s) {
+            const double cost = waves * (4.5 + 1.05 * pages) + last_wave(rest * tiles * s, (pages + s - 1) / s) + 1.7 + (s > 8 ? 2.0 : 0.0) +
+                                1.2e-6 / 6.5 * rest * tiles * s * rows * (kHeadDim + 2) * 4;
+            if (cost < best_cost) {
                 best_cost = cost;
-                best = s > 1 && rest > 0 ? Cut{(int)whole, s, false} : Cut{(int)items, 1, false};
+                best = Cut{(int)whole, s, false};
             }
         }
     }
-    // (a cluster's merge costs about a page and a half)
-    for (int s = 2; full <= 1 && s <= kMostInCluster && s <= pages; ++s) {
-        const int at_once = clusters(s);
-        if (at_once < 1) continue;
-        const long long waves = (items * tiles + at_once - 1) / at_once;
-        const double cost = (double)waves * (6 + (pages + s - 1) / s) + 1.5;
-        if (cost < best_cost - 1e-9) {
+    for (int s = 2; full == 0 && s <= kMostInCluster && s <= pages; ++s) {
+        if (items * tiles > clusters(s)) continue;                      // (one wave of them)
+        const double turns = (int)((rows * 32 / s + kRowTile - 1) / kRowTile);
+        const double cost = last_wave(items * tiles * s, (pages + s - 1) / s) + (s > 8 ? 1.8 + 0.84 * turns : 0.3 + 0.42 * turns);
+        if (cost < best_cost) {
             best_cost = cost;
             best = Cut{0, s, true};
         }

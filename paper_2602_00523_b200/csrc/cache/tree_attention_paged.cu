@@ -25,7 +25,7 @@
 // rate; 80 layers x 16k x 9 nodes sealed: 660 us in a burst, 790 in a loop, at 1.4 to 1.7 GHz, where 415 us of traffic are the floor).  More row tiles: the
 // tensor pipe, 640 clocks a page and tile (384 for the scores of 64 keys, where 128 keys at once would cost 256 a page but need 128 more columns of
 // tensor memory; 256 for P V), of the 800 that a page takes with two blocks (one layer, 60 nodes, 16k keys: 46 us).  Short launches: some 4 000 clocks before
-// the first scores (offsets, page ids, pages, query rows), 1 150 to 1 650 a page, 5 000 for partial results and merge (one token at 2k keys 11.1 us).
+// the first scores (offsets, page ids, pages, query rows), 1 150 to 1 650 a page, 5 000 for partial results and merge (one token at 2k keys 10.8 us).
 // Tried and slower: steps of 128 keys in one S buffer (the softmax waits 2 000 clocks a step for the products of its own block; 80 layers 735 us where
 // pages took 690); a maximum in every page (2 300 clocks a page instead of 1 100 to 1 500); one exponential pair in eight or four on the FMA pipe (+0.5, +3 %).
 #include <cuda_fp16.h>
@@ -926,8 +926,8 @@ static int clusters(int S) {
 //   a wave of blocks, one per SM           2.5 + 0.67 a page (a lone token 7.5 + 0.67 P with the launch's 5: 8.6 / 9.9 / 12.5 / 18.2 / 49.7 for 2 / 4 / 8 / 16 / 63)
 //   ... two per SM                         4.5 + 1.05 a page
 //   the merge as a kernel                  1.7, 2 more beyond eight slices (another round of reads), and the partial results, written and read
-//   the merge in a cluster                 0.3, and 0.42 for each of a thread's outputs (128 rows: 6.7 us with two slices, 1.5 with eight); 1.5 more and twice
-//                                          that beyond eight slices
+//   the merge in a cluster                 0.3, and 0.42 for each of a thread's outputs (128 rows: 6.7 us with two slices, 1.5 with eight), 0.55 beyond eight slices;
+//                                          several clusters of more than ten blocks 1.6 more (one token at 2k keys, 8 / 10 / 11 / 16 slices 11.1 / 10.7 / 11.9 / 11.8)
 // Full waves are left whole and what is left over fills the last one: 640 items of 257 pages are two waves and a sixth.  Cut only for a clear gain, since
 // trees and lengths of a batch differ and blocks without rows leave at once: four sequences of 200 to 800 keys, 24 to 60 nodes, 18.6 us whole, 24 to 28 cut.
 static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
@@ -958,7 +958,7 @@ static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, i
     for (int s = 2; full == 0 && s <= kMostInCluster && s <= pages; ++s) {
         if (items * tiles > clusters(s)) continue;                      // (one wave of them)
         const double turns = (int)((rows * 32 / s + kRowTile - 1) / kRowTile);
-        const double cost = last_wave(items * tiles * s, (pages + s - 1) / s) + (s > 8 ? 1.8 + 0.84 * turns : 0.3 + 0.42 * turns);
+        const double cost = last_wave(items * tiles * s, (pages + s - 1) / s) + 0.3 + (s > 8 ? 0.55 : 0.42) * turns + (s > 10 && items * tiles > 4 ? 1.6 : 0.0);
         if (cost < best_cost) {
             best_cost = cost;
             best = Cut{0, s, true};

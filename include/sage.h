@@ -251,7 +251,8 @@ int sage_compact_kv(void *k_pool, void *v_pool, int64_t layer_stride_elems, int 
  * a node j of the tree at L_b + depth(j); of what sage_tree_attention would let node i see, the keys at positions kappa with
  * pi - kappa < window or kappa < n_sink remain (its own always).  window >= 1, n_sink >= 0; a window of L_b + 64 or more takes nothing away.
  * Only pages that hold such a key are read: page_table entries of the others are not looked at.
- * Softmax and accumulation in fp32, probabilities rounded to bf16.  ws: sage_tree_attention_window_workspace_size(...)
+ * Softmax and accumulation in fp32, probabilities rounded to bf16.  A sequence that is reported for its node count, its length or (below) its
+ * sealed pages is left out, its rows of `out` as they were.  ws: sage_tree_attention_window_workspace_size(...)
  * bytes, for the same sizes.  One or two launches. */
 int sage_tree_attention_window(const void *q, const void *k_pool, const void *v_pool,
                                int64_t layer_stride_elems, int n_layers, int n_pages,

@@ -147,6 +147,14 @@ __device__ __forceinline__ Walk make_walk(int L, int N, int sealed, int window, 
     return k;
 }
 
+// What is wrong with a sequence; 0: nothing.  One with an error is left out, by the merge too.
+__device__ __forceinline__ int sequence_error(const Params& p, int n0, int N, int L, int sealed) {
+    if (N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 > p.sum_nodes - N) return SAGE_STATUS_BAD_TREE;
+    if (L < 0 || (long long)L + N > (long long)p.max_pages * kPageSize || sealed < 0 || sealed > L / kPageSize || sealed > p.max_pages8)
+        return SAGE_STATUS_BAD_PAGE;
+    return 0;
+}
+
 // What a row sees: the slots of the tree, and where its window begins.
 struct Sight {
     uint64_t tree;      // tree slots, one bit each
@@ -439,12 +447,10 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     const int N = p.node_offsets[b + 1] - n0;
     const int L = p.seq_len[b];
     const int sealed = p.sealed ? p.sealed[b] : 0;
-    const bool bad_tree = N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 > p.sum_nodes - N;
-    const bool bad_page = !bad_tree && (L < 0 || (long long)L + N > (long long)p.max_pages * kPageSize || sealed < 0 ||
-                                        sealed > L / kPageSize || sealed > p.max_pages8 || (smem_u32(smem) & 1023));
+    const int error = (smem_u32(smem) & 1023) ? SAGE_STATUS_BAD_PAGE : sequence_error(p, n0, N, L, sealed);
     const int T = L + N, M = N * p.G, row0 = rtile * kRowTile;
-    if (bad_tree || bad_page) {                             // uniform
-        if (tid == 0) report_status(p.status, bad_tree ? SAGE_STATUS_BAD_TREE : SAGE_STATUS_BAD_PAGE);
+    if (error) {                                            // uniform
+        if (tid == 0) report_status(p.status, error);
         return;
     }
     if (row0 >= M) return;
@@ -829,7 +835,7 @@ __global__ void __launch_bounds__(256) paged_merge_kernel(const Params p) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, S = p.n_splits, quad = blockIdx.z * 8 + warp;
     const int item = p.n_whole + blockIdx.y, g = item % p.Hkv, b = item / p.Hkv % p.batch, layer = item / (p.Hkv * p.batch);
     const int n0 = p.node_offsets[b], N = p.node_offsets[b + 1] - n0, M = N * p.G;
-    if (N < 1 || N > SAGE_MAX_NODES || n0 < 0 || n0 > p.sum_nodes - N || blockIdx.x * 32 >= M) return;      // (not worked on)
+    if (sequence_error(p, n0, N, p.seq_len[b], p.sealed ? p.sealed[b] : 0) || blockIdx.x * 32 >= M) return;      // (not worked on)
     const int R = blockIdx.x * 32 + lane;
     const bool ok = R < M;
     const size_t rows = (size_t)p.row_tiles * kRowTile, r = ok ? R : blockIdx.x * 32;

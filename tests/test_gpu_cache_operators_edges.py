@@ -463,3 +463,98 @@ def test_rope_refuses_to_turn_rows_in_place_that_lie_apart():
         sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args)
     with pytest.raises(sage.SageError):
         sage.sage_rope_append(rows[:, :, :4], rows[:, :, 4:5], rows[:, :, 5:], *args, pos=pos, parent=dev32([-1]), next_pos=dev32([0]))
+
+
+def test_calls_on_several_streams_at_once():
+    """Windowed, sealed and plain tree attention, appending and sealing side by side, each with its own workspace."""
+    b = Batch(64, [1500, 200], [20, 9], 32, 8)
+    w_args = window_args(b)
+    s = Batch(65, [1500, 200], [20, 9], 32, 8)
+    s_args = sealed_args(s, s.seal([23, 3]))
+    f = Batch(66, [640, 300], [1, 1], 8, 8)
+    fk, fv, ft = f.pools()
+    pools = [dev16(fk), dev16(fv), dev32(ft), dev32([640, 300])]
+
+    def seal():
+        cache = sage.new_sealed_cache(1, 16, 8, dev32(np.arange(20).reshape(2, 10) % 16))
+        sage.sage_seal_kv(*pools, dev32([0, 0]), cache)
+        return cache["k"].view(torch.uint8)
+
+    calls = [lambda: sage.sage_tree_attention_window(*w_args, 700, 5), lambda: sage.sage_tree_attention_sealed(*s_args),
+             lambda: sage.sage_tree_attention(*w_args), seal, lambda: sage.sage_tree_attention_window(*w_args, 10 ** 6)]
+    alone = [c() for c in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in calls]
+    for _ in range(20):
+        got = []
+        for c, st in zip(calls, streams):
+            with torch.cuda.stream(st):
+                got.append(c())
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(alone, got))
+
+
+def test_scale_bytes_out_of_range_are_read_as_the_nearest():
+    b = Batch(67, [300], [3], 8, 2)
+    args = sealed_args(b, b.seal([4]))
+    out = []
+    for low, high in ((67, 187), (0, 255)):
+        for name in ("k_exp", "v_exp"):
+            args[4][name].fill_(low)
+        args[4]["v_exp"][:, args[4]["page_table"][0, 1]] = high
+        out.append(sage.sage_tree_attention_sealed(*args))
+    assert torch.equal(out[0], out[1]) and torch.isfinite(out[0].float()).all()
+
+
+def test_rope_trees_of_more_than_64_nodes_are_reported():
+    q = torch.ones(1, 70, 4, DIM, dtype=torch.bfloat16, device="cuda")
+    pool = torch.zeros(1, 4, 4, PAGE, DIM, dtype=torch.bfloat16, device="cuda")
+    st, out = sage.new_status(), torch.zeros_like(q)
+    sage.sage_rope_append(q, q, q, sage.make_rope_policy(), pool, pool.clone(), dev32([[0, 1, 2]]), dev32([5]), dev32([0, 65]),
+                          parent=dev32(np.arange(70) - 1), next_pos=dev32([3]), out=out, status=st)
+    torch.cuda.synchronize()
+    assert int(st.item()) == sage.SAGE_STATUS_BAD_TREE and not out.any() and not pool.any()
+
+
+def test_first_calls_inside_a_capture():
+    """In a process of its own, since attributes are set once: nothing that a first call does breaks a capture."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    code = """
+import sys, torch
+sys.path[:0] = [%r, %r]
+import numpy as np
+import paper_2602_00523_b200 as sage
+from cache_reference import Batch
+from test_gpu_cache_operators import SCALE, host, near_sealed, sealed_args
+b = Batch(68, [900], [9], 16, 4)
+args = sealed_args(b, b.seal([14]))
+out = torch.empty_like(args[0])
+need = sage.sage_tree_attention_sealed_workspace_size(1, 1, 9, 16, 4, 128, args[3].shape[1])
+ws = torch.empty(max(16, need), dtype=torch.uint8, device="cuda")
+torch.cuda.synchronize()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    sage.sage_tree_attention_sealed(*args, out=out, ws=ws)
+g.replay()
+torch.cuda.synchronize()
+near_sealed(b, host(out))
+print("sound")
+""" % (root, os.path.join(root, "tests"))
+    got = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert got.returncode == 0 and "sound" in got.stdout, got.stderr[-2000:]
+
+
+@pytest.mark.parametrize("lengths,heads,layers", [([300, 200], (16, 4), 1), ([4000, 5000], (64, 8), 1), ([700, 700], (8, 8), 24), ([130, 130], (8, 8), 20)])
+def test_rows_of_a_reported_sequence_stay_however_the_launch_is_cut(lengths, heads, layers):
+    for at, value in ((5, -1), (6, -2)):        # sealed, length
+        b = Batch(69, lengths, [10, 7], *heads, layers)
+        args = sealed_args(b, b.seal([l // PAGE for l in lengths]))
+        args[at][1] = value
+        st, out = sage.new_status(), torch.full_like(args[0], 3.0)
+        sage.sage_tree_attention_sealed(*args, out=out, status=st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == sage.SAGE_STATUS_BAD_PAGE
+        assert (out[:, 10:] == 3.0).all() and not (out[:, :10] == 3.0).all(-1).any()

@@ -319,9 +319,10 @@ int sage_seal_kv(const void *k_pool, const void *v_pool, int64_t layer_stride_el
 
 /* Tree attention over a cache whose first sealed[b] pages are sealed (0 <= sealed[b] <= L_b / 64) and the rest, with the tree's rows, bf16:
  * as sage_tree_attention in everything else.  Sealed keys and values enter the products as the 8-bit numbers that they are, queries as the
- * sum of two e4m3 numbers (off by 2^-17 of the row's largest element at most) and probabilities as the sum of an e4m3 and an
- * e5m2 number (off by 2^-7 of their value, or by 2^-20 of the row's largest).  Values of a sequence whose scales differ by more than about
- * 2^20 lose precision relative to the largest.  ws: sage_tree_attention_sealed_workspace_size(...)
+ * sum of two e4m3 numbers (off by 2^-17 of the row's largest element at most) and probabilities over sealed keys as the sum of three e5m2 numbers: off by
+ * 2^-8 of their value at most down to 2^-18 of the row's largest probability, by 2^-27 of that below.  Pages are read from the last to the first, and where
+ * the values of one have a scale 2^s below the largest read until then, both limits lie 2^s higher for it: with s up to 18 the largest
+ * probabilities keep their 2^-8, with s = 27 nothing is left of the page.  ws: sage_tree_attention_sealed_workspace_size(...)
  * bytes, for the same sizes.  One or two launches. */
 int sage_tree_attention_sealed(const void *q, const void *k_pool, const void *v_pool,
                                int64_t layer_stride_elems, int n_layers, int n_pages,

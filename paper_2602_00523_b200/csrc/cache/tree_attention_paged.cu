@@ -15,8 +15,11 @@
 //   softmax : one thread per row, online, fp32, log2 domain
 // What is sealed is multiplied as it is, in kind::f8f6f4, without a way through registers and back: each bf16 query row is
 // the sum of two e4m3 rows (split_queries: exact down to 2^-9 of the row's largest element, off by 2^-17 of it below), and each
-// probability the sum of an e4m3 and an e5m2 number (split_four: off by 2^-7 of its value, where bf16 has 2^-8, or by 2^-17 against a
-// reference that lies 2^3 or more below the row's maximum).  Two products of 8 bits cost the tensor pipe what one of 16 does, and HBM half.
+// probability the sum of three e5m2 numbers (split_three: with the rounding to fp16 ahead of it off by less than 2^-8 of its value, which is what bf16 has, for
+// values from 2^-8 on against a reference that lies 2^10 or more below the row's maximum, and by 2^-17 below).  An e4m3 and an e5m2 number, one product less, have
+// 2^-7.9 near the maximum, but 2^-3 from 2^-13 of it on: 2 to 5 % of an output whose row has a key 9 to 11 ahead of thousands (80 layers x 16k x 9 nodes 667 to
+// 707 us with two terms, 738 with three; one layer, 60 nodes 47.3 / 50.0).  Two e5m2 numbers would be off by 2^-7.
+// Two products of 8 bits cost the tensor pipe what one of 16 does: the scores cost the same as those of bf16 keys, P V half as much again, and HBM half.
 // The scales are powers of two: the key's goes into the row's factor of the scores, the value's into the exponent of the
 // probabilities (against the largest of the pages so far, `v_ref`, to which the accumulator is scaled).
 // All waits are bounded: on expiry the block records SAGE_STATUS_TIMEOUT, drains its copies and MMAs, frees its TMEM and returns.
@@ -48,16 +51,18 @@ constexpr uint32_t kIdescPage = idesc_f16(kPageSize);       // S = Q K^T, bf16
 // kind::f8f6f4: D fp32, M = 128; types of A: 0 e4m3, 1 e5m2; B e4m3
 constexpr uint32_t idesc_f8(uint32_t n, uint32_t a_type) { return (1u << 4) | (a_type << 7) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 constexpr uint32_t kIdescSealedQK = idesc_f8(kPageSize, 0);
-constexpr uint32_t kIdescSealedPVHigh = idesc_f8(kHeadDim, 0) | (1u << 16);     // B (= V) MN-major
-constexpr uint32_t kIdescSealedPVLow = idesc_f8(kHeadDim, 1) | (1u << 16);
-// Probabilities are taken against a reference 2^headroom below the maximum that set it, and may reach 448 = 2^8.807 (e4m3's largest): a
-// row's maximum may grow by 2^(8.8 - headroom) before the accumulator is scaled again.  At first, when most of the growth is still to come, a headroom
-// of 3 (a page's maximum may lie 4 below the row's in the scores), later 5.  With 6 throughout, eleven of 65 pages of 16k normally distributed keys
-// had to move some row of their warp, now three.
-constexpr float kHeadroomFirst = 3.f, kHeadroom = 5.f, kMostLog2 = 8.807f;
+constexpr uint32_t kIdescSealedPV = idesc_f8(kHeadDim, 1) | (1u << 16);         // B (= V) MN-major
+// Probabilities are taken against a reference 2^headroom below the maximum that set it, and may reach 2^15.999 (fp16's largest): a
+// row's maximum may grow by 2^(15.9 - headroom) before the accumulator is scaled again.  At first, when most of the growth is still to come, a headroom
+// of 10 (a page's maximum may lie 4 below the row's in the scores), later 12: a row's largest probability is at least 2^10, and what
+// the formats keep of small ones is counted from there.
+constexpr float kHeadroomFirst = 10.f, kHeadroom = 12.f, kMostLog2 = 15.9f;
 constexpr int kEmuPairs = 0;
-constexpr uint32_t kMostF16 = 0x5f00;       // 448 as fp16 bits
-constexpr float kMostSum = 32.f * kMaxSum;  // bf16 pages: what the probabilities of a page may sum to (kMaxSum is against the maximum itself)
+constexpr uint32_t kMostF16 = 0x7bff;       // fp16's largest number
+constexpr float kMostSum = 4096.f * kMaxSum;    // bf16 pages: what the probabilities of a page may sum to (kMaxSum is against the maximum itself)
+constexpr int kTerms = 3;                   // e5m2 numbers that a probability over sealed pages is the sum of
+template <bool kSealed>
+constexpr int kWords = kSealed ? 8 * kTerms : 16;   // of the probabilities of 32 keys: 8 for each term; bf16 16
 // Exponents of sealed scales (sage_seal_kv writes no others; a byte outside is read as the nearest).
 constexpr int kExpLo = 127 - 60, kExpHi = 127 + 60;
 
@@ -105,9 +110,8 @@ __device__ __forceinline__ void mma_ts_f8(uint32_t leader, uint32_t d_tmem, uint
                  ::"r"(d_tmem), "r"(a_tmem), "r"(b_lo), "n"(kHi), "n"(kIdesc), "r"(acc), "r"(leader) : "memory");
 }
 
-// Four fp16 numbers (two words) as a word of e4m3 and one of what is left over, in e4m3 or e5m2.  (The first word is put together
+// Four fp16 numbers (two words) as a word of e4m3 and one of what is left over, in e4m3 too.  (The first word is put together
 // before it is read again: with the 16-bit halves used for both, the compiler of CUDA 12.9 subtracts the wrong one.)
-template <bool kLowE5M2>
 __device__ __forceinline__ void split_four(uint32_t x0, uint32_t x1, uint32_t& high, uint32_t& low) {
     uint32_t b0, b1;
     asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
@@ -116,12 +120,21 @@ __device__ __forceinline__ void split_four(uint32_t x0, uint32_t x1, uint32_t& h
         : "=&r"(b0), "=r"(b1) : "r"(high));
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(b0) : "r"(x0), "r"(b0));
     asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(b1) : "r"(x1), "r"(b1));
-    if constexpr (kLowE5M2)
-        asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e5m2x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e5m2x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
-            : "=r"(low) : "r"(b0), "r"(b1));
-    else
-        asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
-            : "=r"(low) : "r"(b0), "r"(b1));
+    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+        : "=r"(low) : "r"(b0), "r"(b1));
+}
+// Four fp16 numbers that are not negative (two words) as the sum of three e5m2 numbers each.  e5m2 is the upper byte of an fp16 number, so the first term is that
+// byte, the second that of what is left over (both differences are exact), the third the nearest e5m2 number to the rest: three
+// significant bits twice, and then half a step of three more, 2^-9 of the number's binade.  Steps stop at 2^-16: 2^-17 for numbers below 2^-8.
+__device__ __forceinline__ void split_three(uint32_t x0, uint32_t x1, uint32_t& first, uint32_t& second, uint32_t& third) {
+    first = __byte_perm(x0, x1, 0x7531);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x0) : "r"(x0), "r"(x0 & 0xff00ff00u));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x1) : "r"(x1), "r"(x1 & 0xff00ff00u));
+    second = __byte_perm(x0, x1, 0x7531);
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x0) : "r"(x0), "r"(x0 & 0xff00ff00u));
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(x1) : "r"(x1), "r"(x1 & 0xff00ff00u));
+    asm("{\n\t.reg .b16 a, b;\n\tcvt.rn.satfinite.e5m2x2.f16x2 a, %1;\n\tcvt.rn.satfinite.e5m2x2.f16x2 b, %2;\n\tmov.b32 %0, {a, b};\n\t}"
+        : "=r"(third) : "r"(x0), "r"(x1));
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }      // -126 <= e <= 127
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -168,8 +181,8 @@ __device__ __forceinline__ uint64_t visible_page(const Sight& s, int t0, int L) 
     return vis;
 }
 
-// exp2(s * scale + base) of 32 columns; kEmu of every 8 pairs on the FMA pipe.  Probabilities for the products in 16 words at pk (sealed: 8 of
-// e4m3, then 8 of what is left over as e5m2; else bf16), their fp32 sums in acc, sealed: the largest so far, as
+// exp2(s * scale + base) of 32 columns; kEmu of every 8 pairs on the FMA pipe.  Probabilities for the products in kWords words at pk (sealed: 8 of
+// each term, see split_three; else bf16), their fp32 sums in acc, sealed: the largest so far, as
 // fp16 bits, in either half of `most`.
 template <bool kSealed, int kEmu>
 __device__ __forceinline__ void exp_pack(const uint32_t* sr, float scale, float base, uint32_t* pk, uint64_t (&acc)[2], uint32_t& most) {
@@ -203,7 +216,7 @@ __device__ __forceinline__ void exp_pack(const uint32_t* sr, float scale, float 
 #pragma unroll
             for (int i = 0; i < 8; i += 2) most = __vimax3_u16x2(most, f16[i], f16[i + 1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) split_four<true>(f16[2 * i], f16[2 * i + 1], pk[4 * h + i], pk[8 + 4 * h + i]);
+            for (int i = 0; i < 4; ++i) split_three(f16[2 * i], f16[2 * i + 1], pk[4 * h + i], pk[8 + 4 * h + i], pk[16 + 4 * h + i]);
         }
     }
 }
@@ -214,7 +227,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
-
+template <bool kSealed>
+__device__ __forceinline__ void tmem_st_words(uint32_t taddr, const uint32_t* r) {
+    tmem_st16(taddr, r);
+    if constexpr (kSealed)
+        asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};"
+                     ::"r"(taddr + 16), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]) : "memory");
+}
 
 // A page for one query row per thread: 64 scores -> probabilities over the first 16 columns of each 32, running reference m
 // and sum l.  scale: of the scores; dv: exponent by which the page's values exceed the accumulator's.
@@ -259,9 +278,9 @@ static __device__ __noinline__ Running careful_page(const Params& p, Shared* sh,
     uint32_t most = 0;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
-        uint32_t pk[16];
+        uint32_t pk[kWords<kSealed>];
         exp_pack<kSealed, 0>(sr[c], scale, base, pk, acc, most);      // may hold -inf
-        tmem_st16(s_taddr + 32 * c, pk);
+        tmem_st_words<kSealed>(s_taddr + 32 * c, pk);
     }
     float sum_a, sum_b;
     f2_unpack(f2_add(acc[0], acc[1]), sum_a, sum_b);
@@ -271,26 +290,26 @@ static __device__ __noinline__ Running careful_page(const Params& p, Shared* sh,
 }
 
 // Any other page: probabilities are taken against the reference of the pages before, and it shows in them whether it still serves (sealed:
-// none above what e4m3 holds; bf16: by their sum, see kMaxSum).  Returns false, with the scores as they were, where it does not.
+// none above what fp16 holds; bf16: by their sum, see kMaxSum).  Returns false, with the scores as they were, where it does not.
 template <bool kSealed>
 __device__ __forceinline__ bool plain_page(uint32_t s_taddr, float scale, int dv, bool row_ok, float m, float& l) {
-    uint32_t sa[32], sb[32], pk[32], most = 0;
+    uint32_t sa[32], sb[32], pa[kWords<kSealed>], pb[kWords<kSealed>], most = 0;
     uint64_t acc[2] = {};
     tmem_ld32(s_taddr, sa);
     tmem_wait_ld_of(sa);
     tmem_ld32(s_taddr + 32, sb);
     const float base = (float)dv - m;
-    exp_pack<kSealed, kEmuPairs>(sa, scale, base, pk, acc, most);
+    exp_pack<kSealed, kEmuPairs>(sa, scale, base, pa, acc, most);
     tmem_wait_ld_of(sb);
-    exp_pack<kSealed, kEmuPairs>(sb, scale, base, pk + 16, acc, most);
+    exp_pack<kSealed, kEmuPairs>(sb, scale, base, pb, acc, most);
     float sum_a, sum_b;
     f2_unpack(f2_add(acc[0], acc[1]), sum_a, sum_b);
     const float sum = (sum_a + sum_b) * pow2(-dv);
     const bool outgrown = kSealed ? max(most & 0xffffu, most >> 16) > kMostF16 : !(sum < kMostSum);
     if (__any_sync(0xffffffffu, row_ok && outgrown)) return false;
     l += sum;
-    tmem_st16(s_taddr, pk);
-    tmem_st16(s_taddr + 32, pk + 16);
+    tmem_st_words<kSealed>(s_taddr, pa);
+    tmem_st_words<kSealed>(s_taddr + 32, pb);
     tmem_wait_st();
     tc_fence_before();
     return true;
@@ -316,7 +335,7 @@ __device__ __forceinline__ float split_queries(uint8_t* sQ, int r) {
         for (int k = 0; k < 4; ++k) {
             const uint4& s = v[2 * c + (k >> 1)];
             const uint32_t a = k & 1 ? s.z : s.x, b = k & 1 ? s.w : s.y;
-            split_four<false>(pack_f16(__uint_as_float(a << 16) * up, __uint_as_float(a & 0xffff0000u) * up),
+            split_four(pack_f16(__uint_as_float(a << 16) * up, __uint_as_float(a & 0xffff0000u) * up),
                               pack_f16(__uint_as_float(b << 16) * up, __uint_as_float(b & 0xffff0000u) * up), h[k], l[k]);
         }
         uint8_t* at = sQ + r * 128 + ((c ^ (r & 7)) << 4);
@@ -585,11 +604,9 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                 } else {
                     const uint32_t dv = dring_mn + ((s * kSlotBytes + kSealedBytes) >> 4);
 #pragma unroll
-                    for (int ks = 0; ks < 2; ++ks)              // 32 keys
-                        mma_ts_f8<kDescHi, kIdescSealedPVHigh>(leader, o_tmem, a + ks * 32, dv + ((ks * 4096) >> 4), ks > 0 ? 1u : acc);
-#pragma unroll
-                    for (int ks = 0; ks < 2; ++ks)
-                        mma_ts_f8<kDescHi, kIdescSealedPVLow>(leader, o_tmem, a + ks * 32 + 8, dv + ((ks * 4096) >> 4), 1u);
+                    for (int ks = 0; ks < 2 * kTerms; ++ks)     // 32 keys; one term of their probabilities after the other
+                        mma_ts_f8<kDescHi, kIdescSealedPV>(leader, o_tmem, a + (ks & 1) * 32 + (ks >> 1) * 8, dv + (((ks & 1) * 4096) >> 4),
+                                                           ks > 0 ? 1u : acc);
                 }
                 tc_commit(leader, &sh->pv_done);
                 tc_commit(leader, &sh->empty[s]);

@@ -4,7 +4,8 @@ Every function below has the name of the C entry point it calls (include/sage.h)
 takes torch CUDA tensors (PyTorch is used for device memory and streams, nothing
 else), passes raw device pointers and sizes through the C ABI and returns the
 output tensors.  Outputs and workspaces can be passed in (``out=`` dicts /
-``ws=``) so that a caller can keep allocation out of its hot loop; the calls that
+``ws=``) so that a caller can keep allocation out of its hot loop; what a call allocates
+itself belongs to the stream that it goes to (``stream=``, else the current one).  The calls that
 launch kernels are marshalled by the extension ``_native`` (csrc/binding.cpp), which
 returns None when an output is still to be allocated.  ctypes (``lib()``) serves size
 queries, settings and callers that bring raw pointers.  There is no CPU fallback: if
@@ -167,9 +168,24 @@ def sage_expand_topk_workspace_size(rows: int, vocab: int) -> int:
     return int(_lib.sage_expand_topk_workspace_size(rows, vocab))
 
 
-def _need(out: Dict[str, torch.Tensor], name: str, make) -> None:
+def _made(make, stream) -> torch.Tensor:
+    """What ``make`` allocates (and fills) for a call that goes to ``stream``: there and not on the current stream, whose later work
+    may otherwise be given a workspace's bytes while the call still uses them, or fill an output behind the call.  The allocator
+    holds it back, once it has been dropped, until what the current stream does with it has been done too."""
+    if stream is None:
+        return make()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        t = make()
+    if t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
+def _need(out: Dict[str, torch.Tensor], name: str, make, stream) -> None:
     if name not in out:
-        out[name] = make()
+        out[name] = _made(make, stream)
 
 
 def sage_expand_topk(logits: torch.Tensor, k: int, k_entropy: int, *, parent=None, rank=None,
@@ -184,14 +200,14 @@ def sage_expand_topk(logits: torch.Tensor, k: int, k_entropy: int, *, parent=Non
     if code is None:
         rows, vocab = logits.shape
         dev = logits.device
-        _need(o, "topk_idx", lambda: torch.empty((rows, k), dtype=torch.int32, device=dev))
-        _need(o, "topk_logprob", lambda: torch.empty((rows, k), dtype=torch.float32, device=dev))
+        _need(o, "topk_idx", lambda: torch.empty((rows, k), dtype=torch.int32, device=dev), stream)
+        _need(o, "topk_logprob", lambda: torch.empty((rows, k), dtype=torch.float32, device=dev), stream)
         for name in ("entropy_full", "entropy_topk", "alpha", "lse"):
-            _need(o, name, lambda: torch.empty(rows, dtype=torch.float32, device=dev))
+            _need(o, name, lambda: torch.empty(rows, dtype=torch.float32, device=dev), stream)
         if parent is not None:
-            _need(o, "draft_token", lambda: torch.empty(parent.numel(), dtype=torch.int32, device=dev))
+            _need(o, "draft_token", lambda: torch.empty(parent.numel(), dtype=torch.int32, device=dev), stream)
         if ws is None:
-            ws = torch.empty(max(16, sage_expand_topk_workspace_size(rows, vocab)), dtype=torch.uint8, device=dev)
+            ws = _made(lambda: torch.empty(max(16, sage_expand_topk_workspace_size(rows, vocab)), dtype=torch.uint8, device=dev), stream)
         code = _native.expand_topk(logits, k, k_entropy, parent, rank, node_offsets, root_token, o, ws, status, stream, False)
     _check(code, "sage_expand_topk")
     return o
@@ -223,13 +239,13 @@ def sage_select_tree(alpha: torch.Tensor, policy: SagePolicy, *, alpha_row=None,
     if code is None:
         dev = alpha.device
         n = batch if batch is not None else alpha_row.numel() if alpha_row is not None else alpha.numel()
-        _need(o, "template_id", lambda: torch.empty(n, dtype=torch.int32, device=dev))
-        _need(o, "depth_cont", lambda: torch.empty(n, dtype=torch.float32, device=dev))
-        _need(o, "width_cont", lambda: torch.empty(n, dtype=torch.float32, device=dev))
+        _need(o, "template_id", lambda: torch.empty(n, dtype=torch.int32, device=dev), stream)
+        _need(o, "depth_cont", lambda: torch.empty(n, dtype=torch.float32, device=dev), stream)
+        _need(o, "width_cont", lambda: torch.empty(n, dtype=torch.float32, device=dev), stream)
         if handover:
-            _need(o, "next_parent", lambda: torch.full((n * SAGE_MAX_NODES,), -1, dtype=torch.int32, device=dev))
-            _need(o, "next_rank", lambda: torch.zeros(n * SAGE_MAX_NODES, dtype=torch.int32, device=dev))
-            _need(o, "next_node_offsets", lambda: torch.zeros(n + 1, dtype=torch.int32, device=dev))
+            _need(o, "next_parent", lambda: torch.full((n * SAGE_MAX_NODES,), -1, dtype=torch.int32, device=dev), stream)
+            _need(o, "next_rank", lambda: torch.zeros(n * SAGE_MAX_NODES, dtype=torch.int32, device=dev), stream)
+            _need(o, "next_node_offsets", lambda: torch.zeros(n + 1, dtype=torch.int32, device=dev), stream)
         code = _native.select_tree(alpha, alpha_row, batch, policy, o, bank_parent, bank_rank, bank_n_nodes, handover, status, stream)
     _check(code, "sage_select_tree")
     return o
@@ -264,7 +280,7 @@ def sage_update_history(path_len: torch.Tensor, policy: SageHistoryPolicy, windo
 
 def sage_build_ancestor_mask(parent: torch.Tensor, node_offsets: torch.Tensor, *, out=None, status=None, stream=None):
     """Returns int64 [sum_nodes] holding the uint64 bitsets."""
-    anc = out if out is not None else torch.zeros(parent.numel(), dtype=torch.int64, device=parent.device)
+    anc = out if out is not None else _made(lambda: torch.zeros(parent.numel(), dtype=torch.int64, device=parent.device), stream)
     _check(_native.build_ancestor_mask(parent, node_offsets, anc, status, stream), "sage_build_ancestor_mask")
     return anc
 
@@ -280,12 +296,12 @@ def sage_tree_attention(q: torch.Tensor, k_pool: torch.Tensor, v_pool: torch.Ten
     """q bf16 [layers, sum_nodes, Hq, d]; pools bf16 [layers, pages, Hkv, P, d];
     page_table int32 [B, max_pages].  Returns bf16 [layers, sum_nodes, Hq, d]."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(lambda: torch.empty_like(q), stream)
     if ws is None:
         n_layers, sum_nodes, Hq, d = q.shape
         need = sage_tree_attention_workspace_size(n_layers, page_table.shape[0], sum_nodes, Hq, k_pool.shape[2], d,
                                                   page_table.shape[1])
-        ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+        ws = _made(lambda: torch.empty(max(16, need), dtype=torch.uint8, device=q.device), stream)
     _check(_native.tree_attention(q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, out, ws, status, stream),
            "sage_tree_attention")
     return out
@@ -303,12 +319,12 @@ def sage_tree_attention_window(q: torch.Tensor, k_pool: torch.Tensor, v_pool: to
                                window: int, sink: int = 0, *, out=None, ws=None, status=None, stream=None) -> torch.Tensor:
     """sage_tree_attention of rows that see the last ``window`` positions and the first ``sink`` ones only; shapes as there."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(lambda: torch.empty_like(q), stream)
     if ws is None:
         n_layers, sum_nodes, Hq, d = q.shape
         need = sage_tree_attention_window_workspace_size(n_layers, page_table.shape[0], sum_nodes, Hq, k_pool.shape[2], d,
                                                          page_table.shape[1], window, sink)
-        ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+        ws = _made(lambda: torch.empty(max(16, need), dtype=torch.uint8, device=q.device), stream)
     _check(_native.tree_attention_window(q, k_pool, v_pool, page_table, seq_len, parent, node_offsets, sm_scale, window, sink, out, ws,
                                          status, stream), "sage_tree_attention_window")
     return out
@@ -348,7 +364,7 @@ def sage_rope_append(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, policy: 
     any distance (parts of a fused projection's rows).  Returns the turned queries (``out``, contiguous) and writes turned keys, and
     values, behind each sequence's prefix into the pools.  Positions: ``pos`` int32 [3, tokens], or ``parent`` and ``next_pos`` [B]."""
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _made(lambda: torch.empty(q.shape, dtype=q.dtype, device=q.device), stream)
     _check(_native.rope_append(q, k, v, policy, k_pool, v_pool, page_table, seq_len, node_offsets, pos, parent, next_pos, out, status,
                                stream), "sage_rope_append")
     return out
@@ -392,12 +408,12 @@ def sage_tree_attention_sealed(q: torch.Tensor, k_pool: torch.Tensor, v_pool: to
     """sage_tree_attention over a cache whose first ``sealed[b]`` pages lie in ``cache`` and whose others, with the tree's rows, lie
     in the bf16 pools; shapes as there."""
     if out is None:
-        out = torch.empty_like(q)
+        out = _made(lambda: torch.empty_like(q), stream)
     if ws is None:
         n_layers, sum_nodes, Hq, d = q.shape
         need = sage_tree_attention_sealed_workspace_size(n_layers, page_table.shape[0], sum_nodes, Hq, k_pool.shape[2], d,
                                                          page_table.shape[1])
-        ws = torch.empty(max(16, need), dtype=torch.uint8, device=q.device)
+        ws = _made(lambda: torch.empty(max(16, need), dtype=torch.uint8, device=q.device), stream)
     _sealed(_native.tree_attention_sealed(q, k_pool, v_pool, page_table, cache, sealed, seq_len, parent, node_offsets, sm_scale, out, ws,
                                           status, stream), "sage_tree_attention_sealed")
     return out
@@ -427,9 +443,9 @@ def sage_accept(parent, draft_token, target_argmax, node_offsets, max_path: int,
     code = _native.accept(parent, draft_token, target_argmax, node_offsets, max_path, o, status, stream)
     if code is None:
         batch, dev = node_offsets.numel() - 1, parent.device
-        _need(o, "path", lambda: torch.empty((batch, max_path), dtype=torch.int32, device=dev))
-        _need(o, "path_len", lambda: torch.empty(batch, dtype=torch.int32, device=dev))
-        _need(o, "bonus_token", lambda: torch.empty(batch, dtype=torch.int32, device=dev))
+        _need(o, "path", lambda: torch.empty((batch, max_path), dtype=torch.int32, device=dev), stream)
+        _need(o, "path_len", lambda: torch.empty(batch, dtype=torch.int32, device=dev), stream)
+        _need(o, "bonus_token", lambda: torch.empty(batch, dtype=torch.int32, device=dev), stream)
         code = _native.accept(parent, draft_token, target_argmax, node_offsets, max_path, o, status, stream)
     _check(code, "sage_accept")
     return o

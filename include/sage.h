@@ -253,7 +253,8 @@ int sage_compact_kv(void *k_pool, void *v_pool, int64_t layer_stride_elems, int 
  * Only pages that hold such a key are read: page_table entries of the others are not looked at.
  * Softmax and accumulation in fp32, probabilities rounded to bf16.  A sequence that is reported for its node count, its length or (below) its
  * sealed pages is left out, its rows of `out` as they were.  ws: sage_tree_attention_window_workspace_size(...)
- * bytes, for the same sizes.  One or two launches. */
+ * bytes, for the same sizes, are what the call works fastest with; with fewer (16 at least) it cuts its work as they allow, so one
+ * workspace serves calls of all sizes (a call for more nodes may ask for fewer bytes than one for less).  One or two launches. */
 int sage_tree_attention_window(const void *q, const void *k_pool, const void *v_pool,
                                int64_t layer_stride_elems, int n_layers, int n_pages,
                                const int32_t *page_table, int max_pages_per_seq, const int32_t *seq_len,
@@ -323,7 +324,7 @@ int sage_seal_kv(const void *k_pool, const void *v_pool, int64_t layer_stride_el
  * 2^-8 of their value at most down to 2^-18 of the row's largest probability, by 2^-27 of that below.  Pages are read from the last to the first, and where
  * the values of one have a scale 2^s below the largest read until then, both limits lie 2^s higher for it: with s up to 18 the largest
  * probabilities keep their 2^-8, with s = 27 nothing is left of the page.  ws: sage_tree_attention_sealed_workspace_size(...)
- * bytes, for the same sizes.  One or two launches. */
+ * bytes, for the same sizes, or fewer (see sage_tree_attention_window).  One or two launches. */
 int sage_tree_attention_sealed(const void *q, const void *k_pool, const void *v_pool,
                                int64_t layer_stride_elems, int n_layers, int n_pages,
                                const int32_t *page_table, int max_pages_per_seq,

@@ -924,6 +924,12 @@ static bool allow_paged() {
 // Or all items are cut and the slices of a row tile are one cluster, which merges them itself; clusters of S blocks fit the chip
 // `clusters(S)` times at once.
 struct Cut { int whole, splits; bool in_cluster; };
+// Bytes of partial results: of the items that are cut and not merged by a cluster.
+static size_t partial_bytes(const Cut& cut, int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads) {
+    const size_t rest = (size_t)n_layers * batch * n_kv_heads - cut.whole;
+    if (rest == 0 || cut.in_cluster) return 16;
+    return rest * cut.splits * row_tiles_for(sum_nodes, n_q_heads / n_kv_heads) * kRowTile * (kHeadDim + 2) * sizeof(float);
+}
 static int clusters(int S) {
     static std::atomic<int> known[64][kMostInCluster + 1];      // + 1; 0: not asked yet
     int dev = 0;
@@ -953,7 +959,9 @@ static int clusters(int S) {
 //                                          several clusters of more than ten blocks 1.6 more (one token at 2k keys, 8 / 10 / 11 / 16 slices 11.1 / 10.7 / 11.9 / 11.8)
 // Full waves are left whole and what is left over fills the last one: 640 items of 257 pages are two waves and a sixth.  Cut only for a clear gain, since
 // trees and lengths of a batch differ and blocks without rows leave at once: four sequences of 200 to 800 keys, 24 to 60 nodes, 18.6 us whole, 24 to 28 cut.
-static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes) {
+// room: of the workspace; no cut is taken whose partial results it does not hold (a size query asks with all the room there is, and more nodes
+// may need less than fewer: what was allocated for one call has to do for another).
+static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, int pages, int sum_nodes, size_t room) {
     const int nodes = (sum_nodes + batch - 1) / batch, limit = nodes < SAGE_MAX_NODES ? nodes : SAGE_MAX_NODES;
     const long long items = (long long)n_layers * batch * n_kv_heads, tiles = row_tiles_for(nodes, G), slots = 2ll * n_sms;
     const double rows = (double)limit * G / (double)tiles;              // of a tile
@@ -972,9 +980,10 @@ static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, i
         for (int s = 2; s <= kMostSplits && s <= pages && rest * tiles * s <= 4 * slots; ++s) {
             const double cost = waves * (4.5 + 1.05 * pages) + last_wave(rest * tiles * s, (pages + s - 1) / s) + 1.7 + (s > 8 ? 2.0 : 0.0) +
                                 1.2e-6 / 6.5 * rest * tiles * s * rows * (kHeadDim + 2) * 4;
-            if (cost < best_cost) {
+            const Cut cut{(int)whole, s, false};
+            if (cost < best_cost && partial_bytes(cut, n_layers, batch, sum_nodes, n_kv_heads * G, n_kv_heads) <= room) {
                 best_cost = cost;
-                best = Cut{(int)whole, s, false};
+                best = cut;
             }
         }
     }
@@ -989,14 +998,8 @@ static Cut pick_cut(int n_sms, int n_layers, int batch, int n_kv_heads, int G, i
     }
     return best;
 }
-// Bytes of partial results: of the items that are cut and not merged by a cluster.
-static size_t partial_bytes(const Cut& cut, int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads) {
-    const size_t rest = (size_t)n_layers * batch * n_kv_heads - cut.whole;
-    if (rest == 0 || cut.in_cluster) return 16;
-    return rest * cut.splits * row_tiles_for(sum_nodes, n_q_heads / n_kv_heads) * kRowTile * (kHeadDim + 2) * sizeof(float);
-}
 static size_t workspace_size(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int pages) {
-    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, n_q_heads / n_kv_heads, pages, sum_nodes);
+    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, n_q_heads / n_kv_heads, pages, sum_nodes, SIZE_MAX);
     return partial_bytes(cut, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads);
 }
 static bool sizes_ok(int n_layers, int batch, int sum_nodes, int n_q_heads, int n_kv_heads, int max_pages) {
@@ -1046,11 +1049,11 @@ static int run(const void* q, const Pools& pools, const SealedPools* s8, int n_l
     sink = sink < max_pages * kPageSize ? sink : max_pages * kPageSize;
     const int pages = most_pages(max_pages, window, sink);
     if (!sizes_ok(n_layers, batch, sum_nodes, n_q_heads, n_kv_heads, max_pages)) return SAGE_ERR_UNSUPPORTED;
-    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes);
+    if (!ws || ws_bytes < 16 || ((uintptr_t)ws & 15)) return SAGE_ERR_WORKSPACE;
+    const Cut cut = pick_cut(resident_ctas(), n_layers, batch, n_kv_heads, G, pages, sum_nodes, ws_bytes);
     const int tiles = row_tiles_for(sum_nodes, G), rest = n_layers * batch * n_kv_heads - cut.whole;
     const double blocks = ((double)cut.whole + (double)rest * cut.splits) * tiles;
     if (blocks > 2147483647.0) return SAGE_ERR_UNSUPPORTED;
-    if (!ws || ws_bytes < partial_bytes(cut, n_layers, batch, sum_nodes, n_q_heads, n_kv_heads) || ((uintptr_t)ws & 15)) return SAGE_ERR_WORKSPACE;
     CUtensorMap qmap, kmap, vmap, k8map, v8map;
     if (!make_pool_map(&kmap, pools.k, n_layers, pools.n_pages, n_kv_heads, pools.layer_stride) ||
         !make_pool_map(&vmap, pools.v, n_layers, pools.n_pages, n_kv_heads, pools.layer_stride) ||

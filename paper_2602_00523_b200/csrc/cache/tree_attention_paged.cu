@@ -60,6 +60,7 @@ constexpr float kHeadroomFirst = 10.f, kHeadroom = 12.f, kMostLog2 = 15.9f;
 constexpr int kEmuPairs = 0;
 constexpr uint32_t kMostF16 = 0x7bff;       // fp16's largest number
 constexpr float kMostSum = 4096.f * kMaxSum;    // bf16 pages: what the probabilities of a page may sum to (kMaxSum is against the maximum itself)
+constexpr long long kDrainCycles = 4000000000ll;    // for what is in flight when a wait has run out (whatever the waits' own budget)
 constexpr int kTerms = 3;                   // e5m2 numbers that a probability over sealed pages is the sum of
 template <bool kSealed>
 constexpr int kWords = kSealed ? 8 * kTerms : 16;   // of the probabilities of 32 keys: 8 for each term; bf16 16
@@ -78,6 +79,7 @@ struct __align__(8) Shared {
     volatile int abort;
     float k_scale[kSlots];     // of the sealed page in a slot
     int v_exp[kSlots];
+    int issued;                // slots that copies have been asked for (-1: nor the query rows)
     int parent[SAGE_MAX_NODES];
 };
 constexpr int kSmemBytes = kQTileBytes + kSlots * kSlotBytes + 1024;
@@ -492,6 +494,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
         mbar_init(&sh->q_ready, 1);
         mbar_init(&sh->q_split, live_warps);
         sh->abort = 0;
+        sh->issued = -1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     tc_fence_before();
@@ -557,12 +560,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                     }
                     now = next;
                 }
-                if (sh->abort && lane == 0) {
-                    // drain: every issued copy must land before the block may exit
-                    mbar_wait_quiet(&sh->q_ready, 0, p.wait_cycles);
-                    for (int n = max(0, issued - kSlots); n < issued; ++n)
-                        mbar_wait_quiet(&sh->full[n % kSlots], (n / kSlots) & 1, p.wait_cycles);
-                }
+                if (lane == 0) sh->issued = issued;
                 __syncwarp();
             }
         } else if (warp == 5) {
@@ -659,8 +657,6 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
                 ok = values_ready(j + 1);
             }
             tc_commit(leader, &sh->o_full);                     // arrives when every MMA has completed
-            // abort: everything issued must retire before the TMEM and the tiles go away
-            if (!ok && lane == 0) mbar_wait_quiet(&sh->o_full, 0, p.wait_cycles);
             __syncwarp();
         }
         if (p.in_cluster) {
@@ -837,6 +833,16 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     }
     tc_fence_before();
     __syncthreads();
+    if (sh->abort) {
+        // Whichever wait ran out: every copy has to land, and every MMA to retire, before the tiles and the tensor memory go away.
+        if (tid == 0) {
+            for (int n = max(0, sh->issued - kSlots); n < sh->issued; ++n)
+                mbar_wait_quiet(&sh->full[n % kSlots], (n / kSlots) & 1, kDrainCycles);
+            if (sh->issued >= 0) mbar_wait_quiet(&sh->q_ready, 0, kDrainCycles);
+            mbar_wait_quiet(&sh->o_full, 0, kDrainCycles);
+        }
+        __syncthreads();
+    }
     if (warp == 5) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemColumns) : "memory");

@@ -373,9 +373,8 @@ Cache16 cache16(OneDevice& d, PyObject* ko, PyObject* vo, int64_t layers) {
     if (layers > 1 && k.stride(0) != v.stride(0)) fail(PyExc_ValueError, "pools: layers at the same distance in both");
     return {k.data_ptr(), v.data_ptr(), layers > 1 ? k.stride(0) : in_layer, size32(layers), size32(k.size(1)), size32(k.size(2))};
 }
-// A mapping with k, v (e4m3 or bytes), k_exp, v_exp and page_table.
-sage_sealed_cache sealed_cache(OneDevice& d, PyObject* o, int64_t layers, int64_t kv_heads, int64_t page, int64_t dim, int64_t batch) {
-    Tensors c(o);
+// A mapping with k, v (e4m3 or bytes), k_exp, v_exp and page_table; it holds them until it goes.
+sage_sealed_cache sealed_cache(OneDevice& d, Tensors& c, int64_t layers, int64_t kv_heads, int64_t page, int64_t dim, int64_t batch) {
     const auto e4m3 = {at::kFloat8_e4m3fn, at::kByte};
     PyObject *ko = c[N.k], *vo = c[N.v], *ke = c[N.k_exp], *ve = c[N.v_exp], *po = c[N.page_table];
     const at::Tensor& k = d.need(ko, "cache k", e4m3, {layers, -1, kv_heads, page, dim}, false);
@@ -454,7 +453,8 @@ PyObject* seal_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int64_t batch = pt.size(0);
         const int32_t* len = d.i32(a[3], "seq_len", {batch});
         int32_t* sealed = d.i32(a[4], "sealed", {batch});
-        const sage_sealed_cache s8 = sealed_cache(d, a[5], c.layers, c.kv_heads, pool.size(3), pool.size(4), batch);
+        Tensors cache(a[5]);
+        const sage_sealed_cache s8 = sealed_cache(d, cache, c.layers, c.kv_heads, pool.size(3), pool.size(4), batch);
         int32_t* status = d.status(a[6]);
         const On on(d);
         void* stream = stream_of(a[7]);
@@ -524,7 +524,8 @@ PyObject* tree_attention_sealed(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded(n, 14, [&]() -> int {
         Attention t(a[0], a[1], a[2], a[3], a[6], a[7], a[8], a[9], a[10], a[11], a[12]);
         const int32_t* sealed = t.d.i32(a[5], "sealed", {t.batch});
-        const sage_sealed_cache s8 = sealed_cache(t.d, a[4], t.c.layers, t.c.kv_heads, t.page, t.dim, t.batch);
+        Tensors cache(a[4]);
+        const sage_sealed_cache s8 = sealed_cache(t.d, cache, t.c.layers, t.c.kv_heads, t.page, t.dim, t.batch);
         const On on(t.d);
         void* stream = stream_of(a[13]);
         return without_gil([&] {

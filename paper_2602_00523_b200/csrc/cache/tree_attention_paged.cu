@@ -57,7 +57,6 @@ constexpr uint32_t kIdescSealedPV = idesc_f8(kHeadDim, 1) | (1u << 16);         
 // of 10 (a page's maximum may lie 4 below the row's in the scores), later 12: a row's largest probability is at least 2^10, and what
 // the formats keep of small ones is counted from there.
 constexpr float kHeadroomFirst = 10.f, kHeadroom = 12.f, kMostLog2 = 15.9f;
-constexpr int kEmuPairs = 0;
 constexpr uint32_t kMostF16 = 0x7bff;       // fp16's largest number
 constexpr float kMostSum = 4096.f * kMaxSum;    // bf16 pages: what the probabilities of a page may sum to (kMaxSum is against the maximum itself)
 constexpr long long kDrainCycles = 4000000000ll;    // for what is in flight when a wait has run out (whatever the waits' own budget)
@@ -77,8 +76,6 @@ struct __align__(8) Shared {
     uint64_t q_split;          // ... as two e4m3 rows each
     uint32_t tmem_base;
     volatile int abort;
-    float k_scale[kSlots];     // of the sealed page in a slot
-    int v_exp[kSlots];
     int issued;                // slots that copies have been asked for (-1: nor the query rows)
     int parent[SAGE_MAX_NODES];
 };
@@ -149,7 +146,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 struct Walk {
     int n_sink;     // pages with sinks, in front of the window's first
     int w0;         // the window's first page
-    int n_sealed;   // of all that are read; the others follow
+    int n_sealed;   // of all that are read (with sealed pages the window takes nothing away); the others follow
     int n;          // pages
     __device__ __forceinline__ int page(int w) const { return w < n_sink ? w : w - n_sink + w0; }
 };
@@ -157,7 +154,7 @@ __device__ __forceinline__ Walk make_walk(int L, int N, int sealed, int window, 
     Walk k;
     k.w0 = max(0, L - window + 1) / kPageSize;              // the root sees furthest back
     k.n_sink = min((sink + kPageSize - 1) / kPageSize, k.w0);
-    k.n_sealed = min(k.n_sink, sealed) + max(0, sealed - k.w0);
+    k.n_sealed = sealed;
     k.n = k.n_sink + (L + N + kPageSize - 1) / kPageSize - k.w0;
     return k;
 }
@@ -183,13 +180,13 @@ __device__ __forceinline__ uint64_t visible_page(const Sight& s, int t0, int L) 
     return vis;
 }
 
-// exp2(s * scale + base) of 32 columns; kEmu of every 8 pairs on the FMA pipe.  Probabilities for the products in kWords words at pk (sealed: 8 of
+// exp2(s * scale + base) of 32 columns.  Probabilities for the products in kWords words at pk (sealed: 8 of
 // each term, see split_three; else bf16), their fp32 sums in acc, sealed: the largest so far, as
 // fp16 bits, in either half of `most`.
-template <bool kSealed, int kEmu>
+template <bool kSealed>
 __device__ __forceinline__ void exp_pack(const uint32_t* sr, float scale, float base, uint32_t* pk, uint64_t (&acc)[2], uint32_t& most) {
     if constexpr (!kSealed) {
-        exp_chunk<kEmu>(sr, scale, base, pk, acc);
+        exp_chunk<0>(sr, scale, base, pk, acc);
     } else {
         const uint64_t scale2 = f2_pack(scale, scale), base2 = f2_pack(base, base);
 #pragma unroll
@@ -201,17 +198,12 @@ __device__ __forceinline__ void exp_pack(const uint32_t* sr, float scale, float 
             uint32_t f16[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                float p0, p1;
-                if (i < kEmu) {
-                    exp2_pair_fma(x2[i], p0, p1);
-                } else {
-                    float x0, x1;
-                    f2_unpack(x2[i], x0, x1);
-                    p0 = fast_exp2(x0);
-                    p1 = fast_exp2(x1);
-                }
-                x2[i] = f2_pack(p0, p1);
-                f16[i] = pack_f16(p0, p1);
+                float x0, x1;
+                f2_unpack(x2[i], x0, x1);
+                x0 = fast_exp2(x0);
+                x1 = fast_exp2(x1);
+                x2[i] = f2_pack(x0, x1);
+                f16[i] = pack_f16(x0, x1);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) acc[i & 1] = f2_add(acc[i & 1], x2[i]);
@@ -240,7 +232,7 @@ __device__ __forceinline__ void tmem_st_words(uint32_t taddr, const uint32_t* r)
 // A page for one query row per thread: 64 scores -> probabilities over the first 16 columns of each 32, running reference m
 // and sum l.  scale: of the scores; dv: exponent by which the page's values exceed the accumulator's.
 //
-// A page that needs care: the first one, one with keys out of sight, one whose values have a larger scale than those so far (o_factor: what the
+// A page that needs care: the first one, one with keys out of sight (bf16: a sealed page lies within the prefix, and that call has no window), one whose values have a larger scale than those so far (o_factor: what the
 // accumulator is to be multiplied by), one whose probabilities outgrew the reference.  Goes through the maximum.
 struct Running { float m, l; };
 template <bool kSealed>
@@ -250,7 +242,7 @@ static __device__ __noinline__ Running careful_page(const Params& p, Shared* sh,
     tmem_ld32(s_taddr, sr[0]);
     tmem_ld32(s_taddr + 32, sr[1]);
     tmem_wait_ld();
-    if (__any_sync(0xffffffffu, vis != ~0ull)) {
+    if (!kSealed && __any_sync(0xffffffffu, vis != ~0ull)) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) {
             if (!((uint32_t)vis & (1u << i))) sr[0][i] = 0xff800000u;      // -inf
@@ -281,7 +273,7 @@ static __device__ __noinline__ Running careful_page(const Params& p, Shared* sh,
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         uint32_t pk[kWords<kSealed>];
-        exp_pack<kSealed, 0>(sr[c], scale, base, pk, acc, most);      // may hold -inf
+        exp_pack<kSealed>(sr[c], scale, base, pk, acc, most);      // may hold -inf
         tmem_st_words<kSealed>(s_taddr + 32 * c, pk);
     }
     float sum_a, sum_b;
@@ -301,9 +293,9 @@ __device__ __forceinline__ bool plain_page(uint32_t s_taddr, float scale, int dv
     tmem_wait_ld_of(sa);
     tmem_ld32(s_taddr + 32, sb);
     const float base = (float)dv - m;
-    exp_pack<kSealed, kEmuPairs>(sa, scale, base, pa, acc, most);
+    exp_pack<kSealed>(sa, scale, base, pa, acc, most);
     tmem_wait_ld_of(sb);
-    exp_pack<kSealed, kEmuPairs>(sb, scale, base, pb, acc, most);
+    exp_pack<kSealed>(sb, scale, base, pb, acc, most);
     float sum_a, sum_b;
     f2_unpack(f2_add(acc[0], acc[1]), sum_a, sum_b);
     const float sum = (sum_a + sum_b) * pow2(-dv);
@@ -468,7 +460,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
     const int N = p.node_offsets[b + 1] - n0;
     const int L = p.seq_len[b];
     const int sealed = p.sealed ? p.sealed[b] : 0;
-    const int error = (smem_u32(smem) & 1023) ? SAGE_STATUS_BAD_PAGE : sequence_error(p, n0, N, L, sealed);
+    const int error = sequence_error(p, n0, N, L, sealed);
     const int T = L + N, M = N * p.G, row0 = rtile * kRowTile;
     if (error) {                                            // uniform
         if (tid == 0) report_status(p.status, error);
@@ -688,7 +680,7 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
             return e;
         };
         auto packed = [](const Raw& e) { return min(max(e.k, (uint32_t)kExpLo), (uint32_t)kExpHi) | (min(max(e.v, (uint32_t)kExpLo), (uint32_t)kExpHi) << 8); };
-        const bool tree = nb > 0 || cut > 0;                // some page is masked (without a window: bf16 ones only)
+        const bool tree = nb > 0;                           // some page may be masked
         const int first_id = sealed_id(lane), next_id = sealed_id(32 + lane);      // (asked for at once: the set-up is a chain of loads)
         if (tree && r < N) sh->parent[r] = p.parent[n0 + r];
         const Raw first_scales = scales_of(lane, first_id);
@@ -768,13 +760,11 @@ tree_attention_paged_kernel(const Params p, const __grid_constant__ CUtensorMap 
             const uint32_t e = __shfl_sync(0xffffffffu, scales, i & 31);
             const int ve = (int)(e >> 8) - 127;
             const float scale = row_scale * __uint_as_float((e & 0xffu) << 23);
-            const int t0 = cut > 0 ? walk.page(w_hi - 1 - j) * kPageSize : 0;
-            const bool masked = t0 < cut && t0 + kPageSize > p.sink;        // (a sealed page lies within the prefix)
-            if (j == 0 || masked || ve > v_ref || !plain_page<true>(s_taddr + x * 64, scale, ve - v_ref, row_ok, m_ref, l_sum)) {
+            if (j == 0 || ve > v_ref || !plain_page<true>(s_taddr + x * 64, scale, ve - v_ref, row_ok, m_ref, l_sum)) {
                 const int v_max = max(v_ref, ve);
                 const float room = j < 2 ? kHeadroomFirst : kHeadroom;
                 const Running u = careful_page<true>(p, sh, (j - 1) & 1, s_taddr + x * 64, o_taddr, scale, ve - v_max, pow2(v_ref - v_max), row_ok, j == 0, room,
-                                                     masked ? visible_page(sight, t0, L) : ~0ull, m_ref, l_sum);
+                                                     ~0ull, m_ref, l_sum);
                 v_ref = v_max;
                 m_ref = u.m;
                 l_sum = u.l;

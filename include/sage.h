@@ -250,11 +250,15 @@ int sage_compact_kv(void *k_pool, void *v_pool, int64_t layer_stride_elems, int 
  * ones.  The tree node i stands at position pi = L_b + depth(i) (the root has depth 0), a key of the prefix at its logical position,
  * a node j of the tree at L_b + depth(j); of what sage_tree_attention would let node i see, the keys at positions kappa with
  * pi - kappa < window or kappa < n_sink remain (its own always).  window >= 1, n_sink >= 0; a window of L_b + 64 or more takes nothing away.
- * Only pages that hold such a key are read: page_table entries of the others are not looked at.
+ * Only pages that hold such a key are read: page_table entries of the others are not looked at.  Values in a page that is read have to be finite, out of
+ * sight or not; keys out of sight may be anything.
  * Softmax and accumulation in fp32, probabilities rounded to bf16.  A sequence that is reported for its node count, its length or (below) its
  * sealed pages is left out, its rows of `out` as they were.  ws: sage_tree_attention_window_workspace_size(...)
  * bytes, for the same sizes, are what the call works fastest with; with fewer (16 at least) it cuts its work as they allow, so one
- * workspace serves calls of all sizes (a call for more nodes may ask for fewer bytes than one for less).  One or two launches. */
+ * workspace serves calls of all sizes (a call for more nodes may ask for fewer bytes than one for less).  How a launch is cut follows from its sizes, and the
+ * room of the node arrays, the page table's width and the workspace count among them: unlike sage_tree_attention's, the work is not scheduled from the
+ * trees that are there.  Room for more nodes costs time (one layer, 16k keys, nine nodes: 25 us in arrays of nine, 42 in arrays of 64), and
+ * the cut shows in the last digit of an output.  One or two launches. */
 int sage_tree_attention_window(const void *q, const void *k_pool, const void *v_pool,
                                int64_t layer_stride_elems, int n_layers, int n_pages,
                                const int32_t *page_table, int max_pages_per_seq, const int32_t *seq_len,
@@ -319,7 +323,7 @@ int sage_seal_kv(const void *k_pool, const void *v_pool, int64_t layer_stride_el
                  int n_kv_heads, int head_dim, int page_size, int32_t *status, void *stream);
 
 /* Tree attention over a cache whose first sealed[b] pages are sealed (0 <= sealed[b] <= L_b / 64) and the rest, with the tree's rows, bf16:
- * as sage_tree_attention in everything else.  Sealed keys and values enter the products as the 8-bit numbers that they are, queries as the
+ * as sage_tree_attention in everything else but how a launch is cut (see sage_tree_attention_window).  Sealed keys and values enter the products as the 8-bit numbers that they are, queries as the
  * sum of two e4m3 numbers (off by 2^-17 of the row's largest element at most) and probabilities over sealed keys as the sum of three e5m2 numbers: off by
  * 2^-8 of their value at most down to 2^-18 of the row's largest probability, by 2^-27 of that below.  Pages are read from the last to the first, and where
  * the values of one have a scale 2^s below the largest read until then, both limits lie 2^s higher for it: with s up to 18 the largest

@@ -17,18 +17,19 @@
 // the sum of two e4m3 rows (split_queries: exact down to 2^-9 of the row's largest element, off by 2^-17 of it below), and each
 // probability the sum of three e5m2 numbers (split_three: with the rounding to fp16 ahead of it off by less than 2^-8 of its value, which is what bf16 has, for
 // values from 2^-8 on against a reference that lies 2^10 or more below the row's maximum, and by 2^-17 below).  An e4m3 and an e5m2 number, one product less, have
-// 2^-7.9 near the maximum, but 2^-3 from 2^-13 of it on: 2 to 5 % of an output whose row has a key 9 to 11 ahead of thousands (80 layers x 16k x 9 nodes 667 to
-// 707 us with two terms, 738 with three; one layer, 60 nodes 47.3 / 50.0).  Two e5m2 numbers would be off by 2^-7.
+// 2^-7.9 near the maximum, but 2^-3 from 2^-13 of it on: 2 to 5 % of an output whose row has a key 9 to 11 ahead of thousands (80 layers x 16k x 9 nodes, in
+// bursts, 670 us with two terms, 740 with three; one layer, 60 nodes 47 / 49).  Two e5m2 numbers (662 us) would be off by 2^-7, 2.5e-3 in the mean of squares, where three have
+// 0.5e-3 and bf16 1.7e-3.
 // Two products of 8 bits cost the tensor pipe what one of 16 does: the scores cost the same as those of bf16 keys, P V half as much again, and HBM half.
 // The scales are powers of two: the key's goes into the row's factor of the scores, the value's into the exponent of the
 // probabilities (against the largest of the pages so far, `v_ref`, to which the accumulator is scaled).
 // All waits are bounded: on expiry the block records SAGE_STATUS_TIMEOUT, drains its copies and MMAs, frees its TMEM and returns.
 //
 // What bounds it.  One row tile: HBM and, in long launches, the board's power limit (28 layers x 4 sequences, window of 4096: 305 us in a burst, the copy
-// rate; 80 layers x 16k x 9 nodes sealed: 660 us in a burst, 790 in a loop, at 1.4 to 1.7 GHz, where 415 us of traffic are the floor).  More row tiles: the
-// tensor pipe, 640 clocks a page and tile (384 for the scores of 64 keys, where 128 keys at once would cost 256 a page but need 128 more columns of
-// tensor memory; 256 for P V), of the 800 that a page takes with two blocks (one layer, 60 nodes, 16k keys: 46 us).  Short launches: some 4 000 clocks before
-// the first scores (offsets, page ids, pages, query rows), 1 150 to 1 650 a page, 5 000 for partial results and merge (one token at 2k keys 10.8 us).
+// rate; 80 layers x 16k x 9 nodes sealed: 740 to 780 us in a burst, 885 in a loop, where 415 us of traffic are the floor).  More row tiles: the chain
+// of a page, scores, probabilities, product, which the SM's other block fills in part: 1 150 clocks a page and tile, of which the tensor pipe works 640 for a sealed one
+// (256 for the scores, 128 for each term of P V) and 512 for a bf16 one (one layer, 60 nodes, 16k keys: 49 us, tensor pipe at 47 %).  Short launches: some 4 000 clocks before
+// the first scores (offsets, page ids, pages, query rows), 1 150 to 1 650 a page, 5 000 for partial results and merge (one token at 2k keys 11.2 us).
 // Tried and slower: steps of 128 keys in one S buffer (the softmax waits 2 000 clocks a step for the products of its own block; 80 layers 735 us where
 // pages took 690); a maximum in every page (2 300 clocks a page instead of 1 100 to 1 500); one exponential pair in eight or four on the FMA pipe (+0.5, +3 %).
 #include <cuda_fp16.h>

@@ -175,7 +175,8 @@ def _made(make, stream) -> torch.Tensor:
     if stream is None:
         return make()
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+        # (0 is the default stream's handle, of which ExternalStream would make a new stream)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream) if stream.cuda_stream else torch.cuda.default_stream()
     with torch.cuda.stream(stream):
         t = make()
     if t.is_cuda:

@@ -110,3 +110,21 @@ def test_outputs_and_workspaces_lie_in_the_memory_of_the_stream(monkeypatch):
             torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+class Handle:
+    """A stream of another library: no more than its handle."""
+
+    def __init__(self, stream):
+        self.cuda_stream = stream.cuda_stream
+
+
+@pytest.mark.gpu
+def test_streams_that_are_not_torch_s():
+    parent, offsets = torch.tensor([-1, 0, 0, 1], dtype=torch.int32, device="cuda"), torch.tensor([0, 4], dtype=torch.int32, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for stream in (torch.cuda.default_stream(), side):
+        got = sage.sage_build_ancestor_mask(parent, offsets, stream=Handle(stream))
+        torch.cuda.synchronize()
+        assert owner(got) == stream.cuda_stream and got.tolist() == [1, 3, 5, 11]
